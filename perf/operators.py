@@ -179,7 +179,7 @@ def prepare(case, seed):
                 t.zero_()
     if own:   # the handles that a training program keeps beside its tensors, and the records of its norms
         from paper_2412_21124_amd import binding as B
-        s["lists"] = {"grads": B.make_tensor_list(s["grads"], groups=groups)}
+        s["lists"] = {"grads": B.make_tensor_list(s["grads"], groups=groups, num_groups=s["count"])}
         for name in ("to", "w", "m", "v", "copy"):
             if name in s:
                 s["lists"][name] = B.make_tensor_list(s[name], like=s["lists"]["grads"])
