@@ -35,8 +35,8 @@
 extern "C" {
 #endif
 
-/* element type of the gradient rows */
-typedef enum { NT_F32 = 0, NT_BF16 = 1 } nt_dtype;
+/* element type of the gradient rows (NT_F32, NT_BF16) and of the tensors of a list (all three) */
+typedef enum { NT_F32 = 0, NT_BF16 = 1, NT_F16 = 2 } nt_dtype;
 
 /* nt_hyper.flags */
 enum {
@@ -307,6 +307,106 @@ int normtest_resplit(int64_t b, int64_t J, int64_t accum_base, int64_t micro_max
  */
 uint32_t normtest_schedule_flags(int64_t step, int64_t test_interval, int64_t b_k, int64_t b_max,
                                  uint32_t flags);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Lists of tensors.  A model's gradients, weights and moments are many tensors, not one vector.  The calls below take
+ * lists of them, each in one launch or two whatever the number of tensors:
+ *
+ *     normtest_grad_norm       N_g = |s| sqrt(sum of x^2), or |s| max |x|, over the tensors of group g,
+ *                              c_g = min(1, max_norm / (N_g + 1e-6)) and the factor f_g = s c_g
+ *     normtest_clip_grads      x <- f_g x, in place or to a list of its own
+ *     normtest_accumulate      y <- beta y + scale f_g x, and the norm of what is stored in the same pass
+ *     normtest_adamw_tensors   AdamW (Alg. 1's update lines) on scale f_g x
+ *
+ * s is the caller's grad_scale (the inverse of a loss scale, else 1).  A group is any subset of the tensors: all of them for
+ * the global norm, each for itself, one worker's.  Squares are summed in fp64 from the first on, so no finite gradient
+ * overflows or vanishes, in an order that the plan alone fixes: results are reproducible bit for bit.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* One tensor of a list: rows x cols elements, element (r, c) at data + r ld + c.  A contiguous tensor of n elements is one
+ * row of n columns (ld is then ignored).  Any element-aligned address; no two elements may share memory (ld >= cols). */
+typedef struct {
+  void* data;              /* device; may be NULL if rows * cols == 0 */
+  int64_t rows, cols, ld;
+  int32_t dtype;           /* nt_dtype */
+  int32_t group;           /* 0 .. G-1; read by the plan only */
+} nt_tensor;
+
+/* The plan of a list: how its tensors are cut into pieces, and the scratch memory of its norms.  It depends on rows, cols and
+ * group alone and serves every list of the same shapes.  normtest_plan_make fills this record and a host image; the caller copies
+ * upload_bytes of the image to `bytes` of device memory (16-byte aligned) and sets `image`.  The other fields are the library's.
+ * One call at a time may use a plan: its scratch memory belongs to the call until it has run (calls on one stream are in order;
+ * on several streams the caller orders them by events, or makes a plan for each). */
+typedef struct {
+  void* image;             /* device copy of the image, set by the caller */
+  size_t bytes;            /* device memory the image takes */
+  size_t upload_bytes;     /* of its beginning, which the host image holds */
+  int64_t elements;        /* of all tensors */
+  int32_t tensors, groups; /* N, G */
+  uint32_t items[2], slabs[2];
+  uint32_t magic, reserved;
+} nt_plan;
+
+/* Which norm */
+enum { NT_NORM_L2 = 0, NT_NORM_MAX = 1 };
+
+/* The norm of one group.  normtest_clip_grads, normtest_accumulate and normtest_adamw_tensors read it on the device. */
+typedef struct {
+  double norm;             /* |grad_scale| * norm of the group (0 for a group without elements)                       */
+  double coef;             /* min(1, max_norm / (norm + 1e-6)); 1 if max_norm <= 0 or the norm is not finite            */
+  float norm32;            /* norm, rounded                                                                            */
+  float factor;            /* grad_scale * coef, rounded: what a gradient is multiplied by                             */
+  uint32_t status;         /* NT_STATUS_NONFINITE: an element is NaN or infinite; NT_STATUS_ZERO_GRAD_NORM: norm == 0  */
+  int32_t clipped;         /* 1 iff coef < 1                                                                           */
+  int64_t elements;        /* of the group                                                                             */
+} nt_norm;
+
+/* flags of normtest_adamw_tensors */
+enum { NT_SKIP_NONFINITE = 1u };   /* leave the tensors of a group alone whose status has NT_STATUS_NONFINITE */
+
+/* Fill `plan` for N tensors (host array; N may be 0) in G >= 1 groups, and, if `image` is not NULL, the host image of
+ * plan->upload_bytes bytes (8-byte aligned; call once without it to learn the size).  plan->image is left as it is.
+ * NT_ERR_BAD_ARG: a negative size, ld < cols where rows > 1, a group outside 0 .. G-1, G < 1 or N < 0;
+ * NT_ERR_TOO_LARGE: more than 2^43 elements. */
+int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* plan, void* image, size_t image_bytes);
+
+/* Host check of a list before it is copied to the device: the shapes are those of `like` (host arrays of N), addresses are there
+ * and element-aligned, ld >= cols where rows > 1, and every dtype's bit (1 << dtype) is in `dtypes`.  NT_OK, NT_ERR_BAD_ARG or,
+ * for a dtype, NT_ERR_UNSUPPORTED. */
+int normtest_list_check(const nt_tensor* list, const nt_tensor* like, int32_t N, uint32_t dtypes);
+
+/*
+ * In the calls below lists are device-resident arrays of plan->tensors records that passed normtest_list_check (8-byte aligned;
+ * NULL if there are none), read by the kernels only; they and their tensors must not change until the call has run.  norms:
+ * device or pinned-host arrays of plan->groups records, 8-byte aligned.  Everything is enqueued on the stream, kernel launches only;
+ * a graph may capture them.  Returns NT_OK or a negative code; on error nothing was enqueued, except that a failing launch may
+ * follow launches that already succeeded.
+ */
+
+/* Norms of the groups of `grads` (any dtypes), and the coefficients for max_norm (<= 0: no clipping, 1).  A group with a NaN or an
+ * infinity has the norm NaN or infinity, coefficient 1 and NT_STATUS_NONFINITE: a norm that is not a number clips nothing.
+ * grad_scale: finite. */
+int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind, double max_norm, double grad_scale,
+                       nt_norm* norms, void* hip_stream);
+
+/* x <- factor x with the factors of `norms`, rounded once to the type of `out` (NULL: in place; tensors of `out` may be those of
+ * `grads` or lie apart from all of them).  In place, the tensors of a group whose factor is 1 are not touched. */
+int normtest_clip_grads(const nt_plan* plan, const nt_tensor* grads, const nt_tensor* out, const nt_norm* norms,
+                        void* hip_stream);
+
+/* dst <- beta dst + scale factor src (factor: of src_norms, 1 without), in fp32, rounded once to dst's type.  beta == 0: dst is
+ * not read.  dst_norms (may be NULL): norms of the values stored in dst, with kind, max_norm and grad_scale as in
+ * normtest_grad_norm, from the same pass.  src and dst tensors are the same or lie apart. */
+int normtest_accumulate(const nt_plan* plan, const nt_tensor* dst, const nt_tensor* src, double beta, double scale,
+                        const nt_norm* src_norms, int32_t kind, double max_norm, double grad_scale, nt_norm* dst_norms,
+                        void* hip_stream);
+
+/* AdamW on grad_scale * factor * grads (factor: of norms, 1 without), in place on the fp32 lists w, m, v.  copy (may be NULL): a list
+ * of any dtypes that receives the new weights, rounded.  Only the AdamW fields and the step of hyper are read.  The arithmetic is
+ * normtest_adamw_gbar's: fp32 gradients give the same bits.  flags: NT_SKIP_NONFINITE or 0. */
+int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt_tensor* w, const nt_tensor* m,
+                           const nt_tensor* v, const nt_tensor* copy, const nt_hyper* hyper, double grad_scale,
+                           const nt_norm* norms, uint32_t flags, void* hip_stream);
 
 /* Plain streaming copy of `bytes` bytes (device to device, 16-byte aligned, bytes % 16 == 0) with the
  * same load/store instructions as the step kernel: a yardstick for achievable HBM bandwidth and for

@@ -17,7 +17,9 @@ import torch
 
 from . import build as _build
 
-NT_F32, NT_BF16 = 0, 1
+NT_F32, NT_BF16, NT_F16 = 0, 1, 2
+NT_NORM_L2, NT_NORM_MAX = 0, 1
+NT_SKIP_NONFINITE = 1
 NT_DO_STATS, NT_DO_ADAMW, NT_PARTIAL, NT_WRITE_GBAR, NT_COORD_TEST, NT_ONE_PASS = 1, 2, 4, 8, 16, 32
 NT_STATUS_NONFINITE = 1
 NT_STATUS_ZERO_GRAD_NORM = 2
@@ -78,6 +80,28 @@ class nt_layer_stats(ctypes.Structure):
 
 
 LAYER_BYTES = ctypes.sizeof(nt_layer_stats)
+
+
+class nt_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class nt_plan(ctypes.Structure):
+    _fields_ = [("image", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("upload_bytes", ctypes.c_size_t), ("elements", ctypes.c_int64),
+                ("tensors", ctypes.c_int32), ("groups", ctypes.c_int32), ("items", ctypes.c_uint32 * 2), ("slabs", ctypes.c_uint32 * 2),
+                ("magic", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class nt_norm(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_double), ("coef", ctypes.c_double), ("norm32", ctypes.c_float), ("factor", ctypes.c_float),
+                ("status", ctypes.c_uint32), ("clipped", ctypes.c_int32), ("elements", ctypes.c_int64)]
+
+    def as_dict(self) -> dict:
+        return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+NORM_BYTES = ctypes.sizeof(nt_norm)
 
 
 class NormtestError(RuntimeError):
@@ -152,6 +176,15 @@ def lib(path: Optional[str] = None):
         L.normtest_resplit.restype = ctypes.c_int
         L.normtest_schedule_flags.argtypes = [i64, i64, i64, i64, ctypes.c_uint32]
         L.normtest_schedule_flags.restype = ctypes.c_uint32
+        plan, dbl = ctypes.POINTER(nt_plan), ctypes.c_double
+        L.normtest_plan_make.argtypes = [ctypes.POINTER(nt_tensor), ctypes.c_int32, ctypes.c_int32, plan, vp, ctypes.c_size_t]
+        L.normtest_list_check.argtypes = [ctypes.POINTER(nt_tensor), ctypes.POINTER(nt_tensor), ctypes.c_int32, ctypes.c_uint32]
+        L.normtest_grad_norm.argtypes = [plan, vp, ctypes.c_int32, dbl, dbl, vp, vp]
+        L.normtest_clip_grads.argtypes = [plan, vp, vp, vp, vp]
+        L.normtest_accumulate.argtypes = [plan, vp, vp, dbl, dbl, vp, ctypes.c_int32, dbl, dbl, vp, vp]
+        L.normtest_adamw_tensors.argtypes = [plan, vp, vp, vp, vp, vp, ctypes.POINTER(nt_hyper), dbl, vp, ctypes.c_uint32, vp]
+        for name in ("plan_make", "list_check", "grad_norm", "clip_grads", "accumulate", "adamw_tensors"):
+            getattr(L, "normtest_" + name).restype = ctypes.c_int
         L.normtest_calib_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
         L.normtest_calib_copy.restype = ctypes.c_int
         L.normtest_calib_streams.argtypes = [vp, ctypes.c_size_t, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -444,6 +477,267 @@ def read_layers(layers: torch.Tensor, L: Optional[int] = None):
     host = layers.cpu().numpy().tobytes()
     L = len(host) // LAYER_BYTES if L is None else L
     return [nt_layer_stats.from_buffer_copy(host, l * LAYER_BYTES) for l in range(L)]
+
+
+# ---- lists of tensors ------------------------------------------------------------------------
+
+_LIST_DTYPES = {torch.float32: NT_F32, torch.bfloat16: NT_BF16, torch.float16: NT_F16}
+ANY_DTYPE = (1 << NT_F32) | (1 << NT_BF16) | (1 << NT_F16)
+
+
+def _rows_of(t: torch.Tensor):
+    """(rows, columns, row stride, order) of a tensor in memory: one row where its elements are dense.  order names its dimensions from
+    the outermost in memory on, None where that is their own order: only then do elements of tensors of other shapes correspond."""
+    dims = [i for i in range(t.dim()) if t.shape[i] != 1]
+    n = t.numel()
+    if n == 0 or not dims:
+        return 1, n, n, None
+    by_stride = sorted(dims, key=lambda i: -t.stride(i))
+    order = None if by_stride == dims else tuple(by_stride)
+    merged = []   # (size, stride) from the innermost out
+    for i in reversed(by_stride):
+        if merged and t.stride(i) == merged[-1][0] * merged[-1][1]:
+            merged[-1] = (merged[-1][0] * t.shape[i], merged[-1][1])
+        else:
+            merged.append((t.shape[i], t.stride(i)))
+    if merged[0][1] != 1:
+        merged.insert(0, (1, 1))   # a column of single elements
+    if len(merged) == 1:
+        return 1, n, n, order
+    if len(merged) > 2 or merged[1][1] < merged[0][0]:
+        raise ValueError("a tensor of a list must be dense or rows of one stride that do not overlap: got shape %s, strides %s"
+                         % (tuple(t.shape), t.stride()))
+    return merged[1][0], merged[0][0], merged[1][1], order
+
+
+class TensorPlan:
+    """How the tensors of a list are cut into pieces, on the device, with the scratch memory of its norms.  Made by make_tensor_list
+    and shared by the lists made `like` it; one call at a time may use it."""
+
+    def __init__(self, records, count: int, orders, shapes, groups: int, device: torch.device):
+        self.records, self.orders, self.shapes, self.groups, self.device = records, orders, shapes, groups, device
+        self.record = nt_plan()
+        rc = lib().normtest_plan_make(records, count, groups, ctypes.byref(self.record), None, 0)
+        if rc == NT_OK:
+            host = torch.empty(max(8, self.record.upload_bytes), dtype=torch.uint8)
+            rc = lib().normtest_plan_make(records, count, groups, ctypes.byref(self.record), host.data_ptr(), host.numel())
+        if rc != NT_OK:
+            raise NormtestError(rc, "normtest_plan_make")
+        self.image = torch.empty(max(16, self.record.bytes), dtype=torch.uint8, device=device)
+        self.image[:host.numel()].copy_(host)
+        self.record.image = self.image.data_ptr()
+        self.stream = _stream_handle(None, device)
+
+
+class TensorList:
+    """Tensors of one device, as the calls on lists take them: their addresses in a table on the device, and a plan.  The tensors may
+    change their values but not their memory; `refresh` reads their addresses again."""
+
+    def __init__(self, tensors, plan: TensorPlan, records):
+        self.tensors, self.plan = tuple(tensors), plan
+        self._records = records
+        self.table = None
+        self._upload()
+
+    def _upload(self):
+        n = len(self.tensors)
+        rc = lib().normtest_list_check(self._records, self.plan.records, n, ANY_DTYPE)
+        if rc != NT_OK:
+            raise NormtestError(rc, "normtest_list_check")
+        host = torch.frombuffer(bytearray(self._records), dtype=torch.uint8) if n else torch.zeros(8, dtype=torch.uint8)
+        if self.table is None or self.table.numel() != host.numel():
+            self.table = torch.empty(host.numel(), dtype=torch.uint8, device=self.plan.device)
+        self.table.copy_(host)
+        self.addresses = [t.data_ptr() for t in self.tensors]
+        self.dtypes = {t.dtype for t in self.tensors}
+
+    def refresh(self, tensors=None) -> "TensorList":
+        """Reads the tensors' addresses again, or those of other tensors of the same shapes and layouts (gradients that were allocated
+        anew).  Ordered on the current stream."""
+        if tensors is not None:
+            tensors = tuple(tensors)
+            if len(tensors) != len(self.tensors):
+                raise ValueError("the list has %d tensors, got %d" % (len(self.tensors), len(tensors)))
+        else:
+            tensors = self.tensors
+        self._records = _like_records(tensors, self.plan)
+        self.tensors = tensors
+        self._upload()
+        return self
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _check_listed(tensors, device):
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.layout != torch.strided:
+            raise TypeError("a list holds dense torch tensors")
+        if t.dtype not in _LIST_DTYPES:
+            raise TypeError("tensors of a list must be float32, bfloat16 or float16, got %s" % t.dtype)
+        if t.device != device:
+            raise ValueError("the tensors of a list must be on one device: got %s and %s" % (t.device, device))
+    if device.type != "cuda":
+        raise ValueError("lists need device tensors; there is no CPU path")
+
+
+def _like_records(tensors, plan: TensorPlan):
+    """Records of tensors that correspond, element by element in memory, to those the plan was made for."""
+    _check_listed(tensors, plan.device)
+    records = (nt_tensor * len(tensors))()
+    for i, t in enumerate(tensors):
+        want, order = plan.records[i], plan.orders[i]
+        rows, cols, ld, own_order = _rows_of(t)
+        same = (rows, cols) == (want.rows, want.cols)
+        if rows == 1 and cols == want.rows * want.cols:   # dense: in the plan's rows
+            rows, cols, ld, same = want.rows, want.cols, want.cols, True
+        if not same or own_order != order or (order is not None and tuple(t.shape) != plan.shapes[i]):
+            raise ValueError("tensor %d of the list does not lie in memory as the plan's: shape %s, strides %s against %s (make the plan "
+                             "from the list that has row strides)" % (i, tuple(t.shape), t.stride(), plan.shapes[i]))
+        records[i] = nt_tensor(t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], want.group)
+    return records
+
+
+def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, like: Optional[TensorList] = None, device=None) -> TensorList:
+    """The tensors (parameters, gradients, moments: a sequence, on one device) as a list for the calls below.
+
+    groups: a number from 0 on for every tensor, whose norms are then taken group by group (default: one group); num_groups: how many there
+    are, where the last may have no tensor (default: up to the largest number).
+    like: a list of corresponding tensors (same sizes; contiguous, or with the same dimensions in the same order in memory), whose plan and
+    groups are shared: gradients, weights and moments of one model.  Tensors are dense, or rows of one stride (column slices); a plan
+    made from dense tensors does not serve sliced ones.  device: of an empty sequence.
+    Making a list copies its tables to the device and waits for that; make it once and keep it."""
+    tensors = tuple(tensors)
+    if like is not None:
+        if groups is not None or num_groups is not None:
+            raise ValueError("groups are those of the list given as like")
+        if len(tensors) != len(like.tensors):
+            raise ValueError("the lists differ in length: %d and %d tensors" % (len(tensors), len(like.tensors)))
+        return TensorList(tensors, like.plan, _like_records(tensors, like.plan))
+    if not tensors and device is None:
+        raise ValueError("an empty list needs a device")
+    device = tensors[0].device if tensors else torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    _check_listed(tensors, device)
+    groups = [0] * len(tensors) if groups is None else [int(g) for g in groups]
+    if len(groups) != len(tensors) or any(g < 0 for g in groups):
+        raise ValueError("groups must hold a number from 0 on for every tensor")
+    num_groups = max(groups, default=0) + 1 if num_groups is None else int(num_groups)
+    if num_groups <= max(groups, default=0):
+        raise ValueError("num_groups is %d, but a tensor is in group %d" % (num_groups, max(groups, default=0)))
+    records, orders = (nt_tensor * len(tensors))(), []
+    for i, (t, g) in enumerate(zip(tensors, groups)):
+        rows, cols, ld, order = _rows_of(t)
+        records[i] = nt_tensor(t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], g)
+        orders.append(order)
+    plan = TensorPlan(records, len(tensors), orders, [tuple(t.shape) for t in tensors], num_groups, device)
+    return TensorList(tensors, plan, records)
+
+
+def make_norms(lst: TensorList) -> torch.Tensor:
+    """Device memory for the norms of a list's groups (uint8[G * sizeof(nt_norm)])."""
+    return torch.zeros(lst.plan.groups * NORM_BYTES, dtype=torch.uint8, device=lst.plan.device)
+
+
+def norm_views(norms: torch.Tensor) -> dict:
+    """Views of the records on the device, one entry per group: norm, factor (float32), flags (int32: status, clipped)."""
+    words = NORM_BYTES // 4
+    f, i = norms.view(torch.float32).view(-1, words), norms.view(torch.int32).view(-1, words)
+    return {"norm": f[:, 4], "factor": f[:, 5], "flags": i[:, 6:8]}
+
+
+def read_norms(norms: torch.Tensor):
+    """Synchronising read of a device nt_norm array: a list of nt_norm."""
+    host = norms.cpu().numpy().tobytes()
+    return [nt_norm.from_buffer_copy(host, g * NORM_BYTES) for g in range(len(host) // NORM_BYTES)]
+
+
+def _list_call(where: str, plan: TensorPlan, lists, norms, stream, fn, *args):
+    """fn(plan, *args, stream) once the lists are known to be where their tables say, on their device."""
+    for lst in lists:
+        if not isinstance(lst, TensorList):
+            raise TypeError("%s takes lists made by make_tensor_list, got %s" % (where, type(lst).__name__))
+        if lst.plan is not plan:
+            raise ValueError("%s: lists of different plans; make one `like` the other" % where)
+        if [t.data_ptr() for t in lst.tensors] != lst.addresses:
+            raise RuntimeError("%s: a tensor of a list has other memory than when the list was made; call its refresh()" % where)
+    for x in norms:
+        if x is not None and (x.device != plan.device or not x.is_contiguous() or _nbytes(x) < plan.groups * NORM_BYTES):
+            raise ValueError("norms must be the contiguous device memory of %d records on %s (make_norms)" % (plan.groups, plan.device))
+    st = _stream_handle(stream, plan.device)
+    rc = _call(plan.device, fn, ctypes.byref(plan.record), *args, st)
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
+    if st != plan.stream:   # the tables' memory stays until this stream has read them
+        stream = torch.cuda.current_stream(plan.device) if stream is None else stream
+        plan.image.record_stream(stream)
+        for lst in lists:
+            lst.table.record_stream(stream)
+
+
+def _first(where: str, lst) -> TensorPlan:
+    if not isinstance(lst, TensorList):
+        raise TypeError("%s takes lists made by make_tensor_list, got %s" % (where, type(lst).__name__))
+    return lst.plan
+
+
+def normtest_grad_norm(grads: TensorList, norms: Optional[torch.Tensor] = None, *, max_norm: float = 0.0, grad_scale: float = 1.0,
+                       kind: int = NT_NORM_L2, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Enqueue the norms of the list's groups and their clipping factors for max_norm (0: none) on `stream` (default: torch's current
+    stream).  Returns the device memory of the records (norms, or new): read_norms after a sync, norm_views without one."""
+    plan = _first("normtest_grad_norm", grads)
+    if norms is None:
+        norms = make_norms(grads)
+    _list_call("normtest_grad_norm", plan, (grads,), (norms,), stream, lib().normtest_grad_norm, grads.table.data_ptr(), kind, float(max_norm),
+               float(grad_scale), norms.data_ptr())
+    return norms
+
+
+def normtest_clip_grads(grads: TensorList, norms: torch.Tensor, *, out: Optional[TensorList] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Multiply the gradients by their groups' factors, in place or into the list `out` (of any types)."""
+    plan = _first("normtest_clip_grads", grads)
+    _list_call("normtest_clip_grads", plan, (grads,) if out is None else (grads, out), (norms,), stream, lib().normtest_clip_grads,
+               grads.table.data_ptr(), None if out is None else out.table.data_ptr(), norms.data_ptr())
+
+
+def normtest_clip_grad_norm(grads: TensorList, max_norm: float, norms: Optional[torch.Tensor] = None, *, grad_scale: float = 1.0,
+                            kind: int = NT_NORM_L2, out: Optional[TensorList] = None,
+                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Norms and clipping in one call: normtest_grad_norm, then normtest_clip_grads.  Returns the records."""
+    norms = normtest_grad_norm(grads, norms, max_norm=max_norm, grad_scale=grad_scale, kind=kind, stream=stream)
+    normtest_clip_grads(grads, norms, out=out, stream=stream)
+    return norms
+
+
+def normtest_accumulate(dst: TensorList, src: TensorList, *, beta: float = 1.0, scale: float = 1.0,
+                        src_norms: Optional[torch.Tensor] = None, norms: Optional[torch.Tensor] = None, max_norm: float = 0.0,
+                        grad_scale: float = 1.0, kind: int = NT_NORM_L2, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dst <- beta dst + scale src, in fp32, rounded once to dst's types (beta 0: dst is not read).  src_norms: records whose factors
+    multiply src too (every micro-batch clipped by itself).  norms: records that receive the norms of what is stored, as
+    normtest_grad_norm(dst) with max_norm, grad_scale and kind would, from the same pass."""
+    plan = _first("normtest_accumulate", dst)
+    _list_call("normtest_accumulate", plan, (dst, src), (src_norms, norms), stream, lib().normtest_accumulate, dst.table.data_ptr(),
+               src.table.data_ptr() if isinstance(src, TensorList) else None, float(beta), float(scale), _ptr(src_norms), kind, float(max_norm),
+               float(grad_scale), _ptr(norms))
+
+
+def normtest_adamw_tensors(grads: TensorList, w: TensorList, m: TensorList, v: TensorList, hyper: nt_hyper, *,
+                           norms: Optional[torch.Tensor] = None, grad_scale: float = 1.0, copy: Optional[TensorList] = None,
+                           skip_nonfinite: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """AdamW on grad_scale * grads (* the factors of norms, which hold normtest_grad_norm's own grad_scale), in place on the float32
+    lists w, m, v; copy: a list of any types that receives the new weights.  skip_nonfinite: tensors of a group whose norm is not finite
+    are left alone."""
+    where = "normtest_adamw_tensors"
+    plan = _first(where, grads)
+    lists = (grads, w, m, v) if copy is None else (grads, w, m, v, copy)
+    for lst in lists[1:4]:
+        if isinstance(lst, TensorList) and not lst.dtypes <= {torch.float32}:
+            raise ValueError("w, m, v must be lists of float32 tensors")
+    tables = [lst.table.data_ptr() if isinstance(lst, TensorList) else None for lst in lists]
+    _list_call(where, plan, lists, (norms,), stream, lib().normtest_adamw_tensors, *tables[:4], tables[4] if copy is not None else None,
+               ctypes.byref(hyper), float(grad_scale), _ptr(norms), NT_SKIP_NONFINITE if skip_nonfinite else 0)
 
 
 def normtest_clip_coef(gbar_sq: float, max_norm: float) -> float:

@@ -1,5 +1,5 @@
-"""Build ``libnormtest.so`` from ``csrc/normtest.hip`` for gfx950 with hipcc (works without a GPU), and the binding's native call
-path from ``csrc/callpath.cpp`` with g++."""
+"""Build ``libnormtest.so`` from ``csrc/normtest.hip`` and ``csrc/tensors.hip`` for gfx950 with hipcc (works without a GPU), and the
+binding's native call path from ``csrc/callpath.cpp`` with g++."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ import sysconfig
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "normtest.hip")
+TENSORS_SRC = os.path.join(_HERE, "csrc", "tensors.hip")
 LIB = os.path.join(_HERE, "libnormtest.so")
 INCLUDE = os.path.join(ROOT, "include")
 CALLPATH_SRC = os.path.join(_HERE, "csrc", "callpath.cpp")
@@ -17,23 +18,42 @@ CALLPATH_SRC = os.path.join(_HERE, "csrc", "callpath.cpp")
 # code (whole and part tiles, every launch shape) have in common, rely on every fused multiply-add being an explicit one;
 # packed fp32 instructions are disabled for the device pass.
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared", "-ffp-contract=off",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 
 
 def build_library(out: str = LIB, quiet: bool = True) -> str:
-    cmd = ["hipcc", *HIPCC_FLAGS, "-I", INCLUDE]
+    """Both sources at the same time, each to an object of its own, then the library."""
     tmp = out + ".tmp.%d" % os.getpid()
-    cmd += ["-o", tmp, SRC]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n%s\n%s" % (" ".join(cmd), res.stderr))
+    objects, running = [], []
+    for src in (SRC, TENSORS_SRC):
+        objects.append("%s.%s.o" % (tmp, os.path.splitext(os.path.basename(src))[0]))
+        running.append(_start(["hipcc", *HIPCC_FLAGS, "-I", INCLUDE, "-c", "-o", objects[-1], src]))
+    try:
+        said = [_finish(r) for r in running]
+        said.append(_finish(_start(["hipcc", *HIPCC_FLAGS, "-shared", "-o", tmp, *objects])))
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     if not quiet:
         # the host pass does not know the device-only target feature and says so: harmless
-        print("\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l))
+        print("\n".join(l for l in "\n".join(said).splitlines() if "packed-fp32-ops" not in l))
     os.replace(tmp, out)
     return out
+
+
+def _start(cmd):
+    return cmd, subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
+
+
+def _finish(started) -> str:
+    cmd, process = started
+    _, said = process.communicate()
+    if process.returncode != 0:
+        raise RuntimeError("hipcc failed:\n%s\n%s" % (" ".join(cmd), said))
+    return said
 
 
 def callpath_file() -> str:
@@ -65,7 +85,7 @@ def _stale(built: str, *sources: str) -> bool:
 def ensure_built() -> str:
     """Path of the built library; builds it if nothing is there or a source is newer than the build."""
     header = os.path.join(INCLUDE, "normtest.h")
-    if _stale(LIB, SRC, header):
+    if _stale(LIB, SRC, TENSORS_SRC, header):
         build_library()
     return LIB
 

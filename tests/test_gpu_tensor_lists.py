@@ -1,0 +1,461 @@
+"""Calls on lists of tensors against plain 64-bit arithmetic.
+
+Bounds.  Squares are summed in fp64: a norm is off by a few 2^-53 per addition, and additions along one path number some hundreds, so
+1e-12.  A factor is rounded once (2^-24).  A value that is written is scale x + beta y in fp32: the scale's rounding (two where a factor and
+a scale meet, 2^-23), one rounding of beta y and one of the result, then at most half a unit of the type it is stored in.  AdamW:
+the bound of the flat vector's kernels, 1e-6 of the larger of the value and the list's root mean square."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2412_21124_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+HALF_UNIT = {F32: 0.0, BF16: 2.0 ** -8, F16: 2.0 ** -11}     # of the value (8 and 11 significant bits), beyond fp32's own rounding
+SMALLEST = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -24}
+GAP = 5.0
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def carve(shapes, dtypes, seed, offset=0, extra=0, scale=0.1, square=False):
+    """Tensors of normal values inside one buffer per type that is GAP everywhere else: `offset` elements between them, rows `extra` elements
+    apart.  Returns (tensors, check), where check() asserts that nothing between them was written."""
+    g, need = gen(seed), {}
+    places = []
+    for shape, t in zip(shapes, dtypes):
+        r, c = shape if len(shape) == 2 else (1, shape[0])
+        at = need.get(t, 3) + offset
+        places.append((t, at, shape, (c + extra, 1) if len(shape) == 2 else (1,)))
+        need[t] = at + r * (c + extra)
+    buffers = {t: torch.full((n + 64,), GAP, dtype=t, device=DEV) for t, n in need.items()}
+    inside = {t: torch.zeros_like(b, dtype=torch.bool) for t, b in buffers.items()}
+    tensors = []
+    for t, at, shape, strides in places:
+        x = buffers[t].as_strided(shape, strides, at)
+        z = torch.randn(shape, device=DEV, generator=g) * scale
+        x.copy_(z.square_() if square else z)
+        inside[t].as_strided(shape, strides, at).fill_(True)
+        tensors.append(x)
+
+    def check():
+        for t, b in buffers.items():
+            assert bool((b[~inside[t]] == GAP).all())
+    return tensors, check
+
+
+def wide(t):
+    return t.detach().double().cpu().numpy().reshape(-1)
+
+
+def norms_of(tensors, groups, G, kind, scale=1.0):
+    total = [0.0] * G
+    for t, g in zip(tensors, groups):
+        x = np.abs(wide(t))
+        if x.size:
+            total[g] = max(total[g], x.max()) if kind == B.NT_NORM_MAX else math.fsum([total[g], float(np.dot(x, x))])
+    return [abs(scale) * (x if kind == B.NT_NORM_MAX else math.sqrt(x)) for x in total]
+
+
+def check_norms(records, tensors, groups, G, kind=B.NT_NORM_L2, scale=1.0, max_norm=0.0):
+    want = norms_of(tensors, groups, G, kind, scale)
+    got = B.read_norms(records)
+    assert len(got) == G
+    for g, (r, n) in enumerate(zip(got, want)):
+        coef = min(1.0, max_norm / (n + 1e-6)) if max_norm > 0 else 1.0
+        assert abs(r.norm - n) <= 1e-12 * n and abs(r.norm32 - n) <= 1e-7 * n
+        assert abs(r.coef - coef) <= 1e-11 * coef and abs(r.factor - scale * coef) <= 1e-7 * abs(scale) * coef
+        assert r.status == (B.NT_STATUS_ZERO_GRAD_NORM if n == 0 else 0) and r.clipped == (r.coef < 1)
+        assert r.elements == sum(t.numel() for t, h in zip(tensors, groups) if h == g)
+    return got
+
+
+def check_written(y, x, old, beta, scale, roundings=3):
+    """y against beta old + scale x, all arrays in 64 bits but y, which is what was written."""
+    terms = np.abs(beta * old) + np.abs(scale * x)
+    want = beta * old + scale * x
+    t = y.dtype
+    bound = roundings * 2.0 ** -24 * terms
+    bound = bound + (np.abs(want) + bound) * HALF_UNIT[t] + SMALLEST[t]
+    assert (np.abs(wide(y) - want) <= bound).all()
+
+
+SIZES = [
+    [(1,)], [(0,)], [(3,)], [(4,)], [(4095,), (4096,), (4097,)], [(5,), (0,), (100_003,), (1,), (8192,)], [(7, 3)], [(33, 33), (17,)],
+    [(1000, 1)], [(3, 5001), (2, 4096)], [(65, 4095), (300,)], [(1 << 20,), (12_345,)],
+]
+TYPES = [(F32,), (BF16,), (F16,), (BF16, F32, F16)]
+
+
+def cycle(types, shapes):
+    return [types[i % len(types)] for i in range(len(shapes))]
+
+
+@pytest.mark.parametrize("shapes", SIZES, ids=str)
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("kind", [B.NT_NORM_L2, B.NT_NORM_MAX])
+def test_norm(shapes, types, kind):
+    x, untouched = carve(shapes, cycle(types, shapes), 1, offset=1, extra=5)
+    groups = [i % 2 for i in range(len(x))]
+    G = max(groups) + 1
+    lst = B.make_tensor_list(x, groups=groups)
+    for scale, max_norm in [(1.0, 0.0), (1.0, 0.5), (2.0 ** -10, 1e-4), (-0.3, 1e9)]:
+        got = B.normtest_grad_norm(lst, max_norm=max_norm, grad_scale=scale, kind=kind)
+        check_norms(got, x, groups, G, kind, scale, max_norm)
+    untouched()
+
+
+@pytest.mark.parametrize("shapes", SIZES, ids=str)
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("to", [None, (F32,), (BF16,), (F16, F32)], ids=str)
+def test_clip(shapes, types, to):
+    x, untouched = carve(shapes, cycle(types, shapes), 2, offset=1, extra=3)
+    lst = B.make_tensor_list(x)
+    old = [wide(t) for t in x]
+    out, out_untouched = (x, untouched) if to is None else carve(shapes, cycle(to, shapes), 3, offset=2)
+    out_list = None if to is None else B.make_tensor_list(out, like=lst)
+    records = B.normtest_clip_grad_norm(lst, 0.01, grad_scale=0.5, out=out_list)
+    r = B.read_norms(records)[0]
+    factor = 0.5 * min(1.0, 0.01 / (r.norm + 1e-6))
+    for y, a in zip(out, old):
+        check_written(y, a, np.zeros_like(a), 0.0, factor)
+    if to is not None:
+        assert all((wide(t) == a).all() for t, a in zip(x, old))
+    untouched()
+    out_untouched()
+
+
+@pytest.mark.parametrize("shapes", SIZES, ids=str)
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("to", [(F32,), (BF16,), (F16, F32)], ids=str)
+@pytest.mark.parametrize("beta", [0.0, 1.0, -0.75])
+def test_accumulate(shapes, types, to, beta):
+    x, x_untouched = carve(shapes, cycle(types, shapes), 4, offset=1, extra=3)
+    y, y_untouched = carve(shapes, cycle(to, shapes), 5, offset=3, extra=7)
+    src = B.make_tensor_list(x, groups=[0] * len(x))
+    dst = B.make_tensor_list(y, like=src)
+    old = [(wide(a), wide(b)) for a, b in zip(x, y)]
+    if beta == 0.0:
+        for t in y:
+            t.fill_(float("nan"))   # not read
+    norms = B.make_norms(dst)
+    for kind in (B.NT_NORM_L2, B.NT_NORM_MAX):
+        B.normtest_accumulate(dst, src, beta=beta, scale=0.25, norms=norms, max_norm=0.5, grad_scale=3.0, kind=kind)
+        if kind == B.NT_NORM_L2:
+            for t, (a, b) in zip(y, old):
+                check_written(t, a, b, beta, 0.25)
+        check_norms(norms, y, [0] * len(y), 1, kind, 3.0, 0.5)
+    x_untouched()
+    y_untouched()
+
+
+def test_accumulate_with_the_factors_of_every_group():
+    shapes = [(4096,), (10_001,), (50, 70), (3,)]
+    x, _ = carve(shapes, [BF16] * 4, 6)
+    groups = [0, 1, 1, 0]
+    src = B.make_tensor_list(x, groups=groups)
+    y, _ = carve(shapes, [F32] * 4, 7)
+    old = [wide(t) for t in y]
+    dst = B.make_tensor_list(y, like=src)
+    norms = B.normtest_grad_norm(src, max_norm=1.0)
+    B.normtest_accumulate(dst, src, scale=0.5, src_norms=norms)
+    r = B.read_norms(norms)
+    assert all(x.clipped for x in r)
+    for t, a, b, g in zip(y, x, old, groups):
+        check_written(t, wide(a), b, 1.0, 0.5 * r[g].coef, roundings=4)
+
+
+def hyper(step=3, **kw):
+    return B.make_hyper(**dict(dict(lr=1e-3, weight_decay=0.1, step=step), **kw))
+
+
+def check_adamw(got, before, grads, h, factor):
+    """(w, m, v) as written against Alg. 1's update lines in 64 bits."""
+    w, m, v = before
+    g = factor * grads
+    m = h.beta1 * m + (1 - h.beta1) * g
+    v = h.beta2 * v + (1 - h.beta2) * g * g
+    w = w * (1 - h.lr * h.weight_decay) - h.lr * (m / (1 - h.beta1 ** h.step)) / (np.sqrt(v / (1 - h.beta2 ** h.step)) + h.eps)
+    for y, want in zip(got, (w, m, v)):
+        if want.size:
+            rms = math.sqrt(float(np.mean(want * want)))
+            assert (np.abs(y - want) <= 1e-6 * np.maximum(np.abs(want), rms)).all()
+
+
+def state(shapes, extra=0):
+    out = [carve(shapes, [F32] * len(shapes), s, offset=s % 3, extra=extra, scale=0.02, square=s == 13) for s in (11, 12, 13)]
+    return [t for t, _ in out], [c for _, c in out]
+
+
+@pytest.mark.parametrize("shapes", SIZES, ids=str)
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("copy", [None, (BF16,), (F16, F32)], ids=str)
+def test_adamw(shapes, types, copy):
+    x, x_untouched = carve(shapes, cycle(types, shapes), 8, offset=1, extra=3)
+    (w, m, v), checks = state(shapes, extra=1)
+    grads = B.make_tensor_list(x)
+    lists = [B.make_tensor_list(t, like=grads) for t in (w, m, v)]
+    c, c_untouched = carve(shapes, cycle(copy, shapes), 9, offset=1) if copy else (None, None)
+    before = [np.concatenate([wide(t) for t in ts]) for ts in (w, m, v)]
+    g = np.concatenate([wide(t) for t in x])
+    h = hyper()
+    norms = B.normtest_grad_norm(grads, max_norm=0.7, grad_scale=0.5)
+    B.normtest_adamw_tensors(grads, *lists, h, norms=norms, grad_scale=2.0, copy=B.make_tensor_list(c, like=grads) if copy else None)
+    factor = 2.0 * 0.5 * B.read_norms(norms)[0].coef
+    check_adamw([np.concatenate([wide(t) for t in ts]) for ts in (w, m, v)], before, g, h, factor)
+    for a, b in zip(c or [], w):
+        assert torch.equal(a, b.to(a.dtype))
+    for check in [x_untouched, *checks, *([c_untouched] if copy else [])]:
+        check()
+
+
+def test_adamw_has_the_bits_of_the_flat_vectors_kernels():
+    n = 3 * 4096 + 1237
+    flat = [torch.randn(n, device=DEV, generator=gen(s)) * 0.02 for s in range(4)]
+    flat[3].square_()
+    flat[3][:50] *= 1e-34   # second moments far below fp32's normal range, too
+    want = [t.clone() for t in flat]
+    h = hyper(step=7)
+    B.normtest_adamw_gbar(want[0], *want[1:], h, 0.37)
+    cuts = [0, 1, 5000, 5003, n]
+    lists = [[t[a:b] for a, b in zip(cuts, cuts[1:])] for t in flat]
+    grads = B.make_tensor_list(lists[0])
+    B.normtest_adamw_tensors(grads, *[B.make_tensor_list(t, like=grads) for t in lists[1:]], h, grad_scale=0.37)
+    for a, b in zip(flat[1:], want[1:]):
+        assert torch.equal(a, b)
+
+
+def test_groups_without_tensors_and_without_elements():
+    x = [torch.zeros(0, device=DEV), torch.full((10,), 2.0, device=DEV), torch.zeros(7, device=DEV)]
+    lst = B.make_tensor_list(x, groups=[1, 3, 4])
+    got = check_norms(B.normtest_grad_norm(lst, max_norm=1.0), x, [1, 3, 4], 5, max_norm=1.0)
+    assert [r.elements for r in got] == [0, 0, 0, 10, 7] and [r.status for r in got] == [2, 2, 2, 0, 2]
+    r = check_norms(B.normtest_grad_norm(B.make_tensor_list(x, groups=[0, 1, 0], num_groups=4)), x, [0, 1, 0], 4)
+    assert [q.elements for q in r] == [7, 10, 0, 0]
+    empty = B.make_tensor_list([], device=DEV)
+    assert check_norms(B.normtest_clip_grad_norm(empty, 1.0), [], [], 1)[0].coef == 1.0
+    B.normtest_accumulate(empty, empty, norms=B.make_norms(empty))
+    B.normtest_adamw_tensors(empty, empty, empty, empty, hyper())
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("types", [F32, BF16, F16])
+def test_the_whole_range_of_a_type(types):
+    """Largest values, whose squares do not fit 32 bits, and smallest ones, whose squares vanish there."""
+    info = torch.finfo(types)
+    for value in (info.max, info.tiny, info.smallest_normal / 4):
+        x = [torch.full((n,), value, dtype=types, device=DEV) for n in (5000, 3)]
+        v = float(x[0][0].double())
+        assert v > 0
+        for kind, want in ((B.NT_NORM_L2, v * math.sqrt(5003)), (B.NT_NORM_MAX, v)):
+            r = B.read_norms(B.normtest_grad_norm(B.make_tensor_list(x), max_norm=1.0, kind=kind))[0]
+            assert abs(r.norm - want) <= 1e-12 * want and r.status == 0
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("types", [F32, BF16, F16])
+@pytest.mark.parametrize("kind", [B.NT_NORM_L2, B.NT_NORM_MAX])
+def test_a_value_that_is_not_finite(bad, types, kind):
+    x = [(torch.randn(n, device=DEV, generator=gen(n)) * 0.1).to(types) for n in (5000, 4097, 70_000)]
+    x[1][4096] = bad
+    lst = B.make_tensor_list(x, groups=[0, 1, 2])
+    norms = B.normtest_grad_norm(lst, max_norm=0.5, grad_scale=0.25, kind=kind)
+    r = B.read_norms(norms)
+    assert [q.status for q in r] == [0, B.NT_STATUS_NONFINITE, 0] and [q.clipped for q in r] == [q.norm > 0.5 and math.isfinite(q.norm) for q in r]
+    assert math.isnan(r[1].norm) if math.isnan(bad) else r[1].norm == math.inf
+    assert (r[1].coef, r[1].factor) == (1.0, 0.25)
+    (w, m, v), _ = state([(5000,), (4097,), (70_000,)])
+    before = [[t.clone() for t in ts] for ts in (w, m, v)]
+    lists = [B.make_tensor_list(t, like=lst) for t in (w, m, v)]
+    B.normtest_adamw_tensors(lst, *lists, hyper(), norms=norms, skip_nonfinite=True)
+    for ts, old in zip((w, m, v), before):
+        assert torch.equal(ts[1], old[1]) and not torch.equal(ts[0], old[0]) and not torch.equal(ts[2], old[2])
+        assert all(bool(torch.isfinite(t).all()) for t in ts)
+    B.normtest_adamw_tensors(lst, *lists, hyper(), norms=norms)
+    assert not bool(torch.isfinite(m[1]).all()) and bool(torch.isfinite(m[2]).all())
+
+
+def test_in_place_with_a_factor_of_one_leaves_every_bit():
+    x = torch.randn(10_000, device=DEV, generator=gen(1))
+    x[17] = math.nan
+    y = x.clone()
+    B.normtest_clip_grad_norm(B.make_tensor_list([x]), 1.0)     # not a number: clips nothing
+    assert torch.equal(x.view(torch.int32), y.view(torch.int32))
+
+
+def test_layouts_that_are_dense_in_another_order():
+    a = torch.randn(130, 70, device=DEV, generator=gen(2))
+    grads = B.make_tensor_list([a.t()])
+    check_norms(B.normtest_grad_norm(grads), [a], [0], 1)
+    out = torch.zeros(130, 70, device=DEV)
+    B.normtest_clip_grads(grads, B.normtest_grad_norm(grads, grad_scale=2.0), out=B.make_tensor_list([out.t()], like=grads))
+    assert torch.equal(out, 2 * a)
+    with pytest.raises(ValueError, match="does not lie in memory"):
+        B.make_tensor_list([torch.zeros(70, 130, device=DEV)], like=grads)
+
+
+def test_long_lists():
+    """Past 2^23 elements the norm has items of its own; slabs and groups of many items."""
+    shapes = [(3_000_001,), (9000, 1100), (5,), (12_000_000,)]
+    x, untouched = carve(shapes, [BF16, F32, F32, F16], 20, offset=1, extra=9)
+    for groups in ([0, 0, 0, 0], [0, 1, 0, 2]):
+        lst = B.make_tensor_list(x, groups=groups)
+        assert lst.plan.record.items[1] > 0
+        for kind in (B.NT_NORM_L2, B.NT_NORM_MAX):
+            check_norms(B.normtest_grad_norm(lst, max_norm=1.0, kind=kind), x, groups, max(groups) + 1, kind, 1.0, 1.0)
+    y, y_untouched = carve(shapes, [F32] * 4, 21)
+    norms = B.make_norms(lst)
+    B.normtest_accumulate(B.make_tensor_list(y, like=lst), lst, beta=0.0, norms=norms)
+    for a, b in zip(x, y):
+        assert torch.equal(a.float(), b)
+    check_norms(norms, y, groups, 3)
+    untouched()
+    y_untouched()
+
+
+def test_elements_past_32_bits():
+    """One tensor of more than 2^32 elements, which takes two launches: its ends, the seam and the total."""
+    n = (1 << 32) + 4099
+    x = torch.ones(n, dtype=BF16, device=DEV)
+    marks = [0, (1 << 31) - 1, 1 << 31, (1 << 32) - 1, 1 << 32, n - 4, n - 1]
+    for i, at in enumerate(marks):
+        x[at] = 2.0 + i
+    lst = B.make_tensor_list([x])
+    total = n - len(marks) + sum((2.0 + i) ** 2 for i in range(len(marks)))
+    r = B.read_norms(B.normtest_clip_grad_norm(lst, 0.5 * math.sqrt(total)))[0]
+    assert abs(r.norm - math.sqrt(total)) <= 1e-12 * r.norm and r.elements == n
+    for i, at in enumerate(marks):
+        assert float(x[at]) == (2.0 + i) / 2
+    assert int((x != 0.5).sum()) == len(marks)
+    norms = B.make_norms(lst)
+    B.normtest_accumulate(lst, lst, beta=0.0, scale=2.0, norms=norms)
+    assert abs(B.read_norms(norms)[0].norm - math.sqrt(total)) <= 1e-12 * r.norm and int((x != 1.0).sum()) == len(marks)
+
+
+def test_the_same_bits_again_and_counters_back_at_zero():
+    shapes = [(1 << 20,), (777_777,), (300, 4000)]
+    x, _ = carve(shapes, [BF16, F32, F16], 30, extra=2)
+    lst = B.make_tensor_list(x, groups=[0, 1, 0])
+    image = lst.plan.image[:lst.plan.record.upload_bytes].clone()
+    first = B.normtest_grad_norm(lst, max_norm=1.0).clone()
+    for _ in range(20):
+        assert torch.equal(B.normtest_grad_norm(lst, max_norm=1.0), first)
+    assert torch.equal(lst.plan.image[:lst.plan.record.upload_bytes], image)
+
+
+def test_streams_and_graphs():
+    shapes = [(50_000,), (70, 900), (3,)]
+    x, _ = carve(shapes, [BF16, F32, F16], 40, extra=2)
+    y, _ = carve(shapes, [F32] * 3, 41)
+    src = B.make_tensor_list(x, groups=[0, 1, 0])
+    dst = B.make_tensor_list(y, like=src)
+    norms, after = B.make_norms(src), B.make_norms(src)
+
+    def step():
+        B.normtest_grad_norm(src, norms, max_norm=1.0)
+        B.normtest_accumulate(dst, src, beta=0.5, src_norms=norms, norms=after, max_norm=1.0)
+        B.normtest_clip_grads(dst, after)
+    start = [t.clone() for t in y]
+    step()
+    want = [t.clone() for t in y], norms.clone(), after.clone()
+    side = torch.cuda.Stream()
+    for t, s in zip(y, start):
+        t.copy_(s)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(y, want[0])) and torch.equal(after, want[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        for t, s in zip(y, start):
+            t.copy_(s)
+        norms.zero_()
+        after.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(y, want[0])) and torch.equal(norms, want[1]) and torch.equal(after, want[2])
+        B.normtest_grad_norm(src)   # an eager call between the replays
+    torch.cuda.synchronize()
+
+
+def test_lists_on_two_streams_at_the_same_time():
+    x = [torch.randn(2_000_003, device=DEV, generator=gen(s)) for s in (1, 2)]
+    lists = [B.make_tensor_list([t]) for t in x]
+    records = [B.make_norms(lst) for lst in lists]
+    streams = [torch.cuda.Stream() for _ in x]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for lst, r, s in zip(lists, records, streams):
+            B.normtest_grad_norm(lst, r, stream=s)
+    torch.cuda.synchronize()
+    for t, r in zip(x, records):
+        check_norms(r, [t], [0], 1)
+
+
+def test_refresh_and_moved_memory():
+    params = [torch.randn(100, device=DEV), torch.randn(5000, device=DEV)]
+    lst = B.make_tensor_list(params)
+    params[1].data = torch.ones(5000, device=DEV)
+    with pytest.raises(RuntimeError, match="refresh"):
+        B.normtest_grad_norm(lst)
+    check_norms(B.normtest_grad_norm(lst.refresh()), params, [0, 0], 1)
+    others = [torch.full((100,), 2.0, dtype=BF16, device=DEV), torch.ones(5000, device=DEV)]
+    check_norms(B.normtest_grad_norm(lst.refresh(others)), others, [0, 0], 1)
+    with pytest.raises(ValueError):
+        lst.refresh([others[0]])
+    with pytest.raises(ValueError):
+        lst.refresh([others[1], others[0]])
+
+
+def test_lists_that_do_not_belong_together_are_refused():
+    a = [torch.zeros(100, device=DEV), torch.zeros(8, 16, device=DEV)]
+    lst = B.make_tensor_list(a)
+    other = B.make_tensor_list([t.clone() for t in a])
+    norms = B.make_norms(lst)
+    h = hyper()
+    with pytest.raises(ValueError, match="different plans"):
+        B.normtest_accumulate(lst, other)
+    with pytest.raises(ValueError, match="different plans"):
+        B.normtest_adamw_tensors(lst, lst, lst, other, h)
+    half = B.make_tensor_list([t.to(BF16) for t in a], like=lst)
+    with pytest.raises(ValueError, match="float32"):
+        B.normtest_adamw_tensors(lst, half, lst, lst, h)
+    with pytest.raises(TypeError, match="make_tensor_list"):
+        B.normtest_accumulate(lst, a)
+    for bad in (norms[:-1], norms.cpu(), torch.zeros(80, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(ValueError, match="norms"):
+            B.normtest_grad_norm(lst, bad)
+    with pytest.raises(ValueError, match="groups"):
+        B.make_tensor_list(a, groups=[0, 1], like=lst)
+    with pytest.raises(ValueError, match="groups"):
+        B.make_tensor_list(a, num_groups=1, like=lst)
+    for n in (0, 1):
+        with pytest.raises(ValueError, match="num_groups"):
+            B.make_tensor_list(a, groups=[0, 1], num_groups=n)
+    for groups in ([0], [0, -1]):
+        with pytest.raises(ValueError, match="groups"):
+            B.make_tensor_list(a, groups=groups)
+    with pytest.raises(ValueError):
+        B.make_tensor_list([a[0]], like=lst)
+    with pytest.raises(ValueError, match="one device"):
+        B.make_tensor_list([a[0], torch.zeros(3)])
+    with pytest.raises(ValueError, match="does not lie in memory"):
+        B.make_tensor_list([a[0], torch.zeros(8, 20, device=DEV)[:, :16]], like=lst)
+    for kw in (dict(max_norm=math.nan), dict(grad_scale=math.inf), dict(kind=5)):
+        with pytest.raises(B.NormtestError):
+            B.normtest_grad_norm(lst, norms, **kw)
+    with pytest.raises(B.NormtestError):
+        B.normtest_adamw_tensors(lst, lst, lst, lst, h, skip_nonfinite=True)
