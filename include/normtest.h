@@ -343,7 +343,7 @@ typedef struct {
   size_t upload_bytes;     /* of its beginning, which the host image holds */
   int64_t elements;        /* of all tensors */
   int32_t tensors, groups; /* N, G */
-  uint32_t items[2], slabs[2];
+  uint32_t items[2], slots[2], slabs[2];
   uint32_t magic, reserved;
 } nt_plan;
 

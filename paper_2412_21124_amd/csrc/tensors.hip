@@ -7,8 +7,9 @@
 //
 // Norms.  x^2 is formed and summed in fp64, so no finite value overflows and no rounding of the sum is seen; the largest
 // magnitude is the largest |x| by its bits as an integer, where a NaN is larger than infinity and so survives.  A block leaves
-// one partial; the blocks of a slab of items count themselves, the last one adds the slab's partials up, and the last slab of a group
-// the group's slabs, and writes its record: one launch, no floating-point atomics, sums in an order that the plan alone fixes.
+// one partial for every group that it meets; the blocks of a slab of partials count themselves, the last one adds the slab up, and the
+// last slab of a group the group's slabs, and writes its record: one launch, no floating-point atomics, sums in an order that the plan
+// alone fixes.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -19,12 +20,40 @@
 
 #include "normtest.h"
 
-#define NT_ITEM 4096            // elements of an item: four per thread of a block of the kernels that write
-#define NT_THREADS 1024         // threads of those
+#define NT_ITEM 4096            // elements of an item of the kernels that write
+#ifndef NT_THREADS
+#define NT_THREADS 256          // threads of a block of the update
+#endif
+#ifndef NT_ADAMW_THREADS
+#define NT_ADAMW_THREADS 512
+#endif
 #define NT_NORM_THREADS 256     // threads of a block of the norm's kernel
-#define NT_LONG_ITEM 32768      // elements of its items in a long list
+#define NT_NORM_FLIGHT 4        // 16-byte loads that a thread of it has in flight
+#define NT_LONG_ITEM 8192       // elements of its items in a long list
+#define NT_LONG_BLOCKS 1024     // and its blocks, which walk such a list
 #define NT_LONG_LIST (1ll << 23)   // elements from which a list is long
 #define NT_MOST_BLOCKS (1u << 20)  // blocks of one launch
+#ifndef NT_ADAMW_LAUNCH
+#define NT_ADAMW_LAUNCH NT_MOST_BLOCKS
+#endif
+#ifndef UPD_NT_X
+#define UPD_NT_X false
+#endif
+#ifndef UPD_NT_Y
+#define UPD_NT_Y false
+#endif
+#ifndef ADAMW_NT_G
+#define ADAMW_NT_G false
+#endif
+#ifndef ADAMW_NT_S
+#define ADAMW_NT_S false
+#endif
+#ifndef NT_ADAMW_LDS
+#define NT_ADAMW_LDS 0
+#endif
+// Elements from which loads (and stores) go past the 256 MB cache that the chip's memory has, because what they touch would not stay in it
+// until it is needed again.
+#define NT_STREAM_NORM (1ll << 27)
 #define NT_PLAN_MAGIC 0x4e54504cu
 #define NT_COUNTER_WORDS 16     // a counter has 64 bytes of its own, so that counting blocks of different slabs do not meet
 
@@ -52,17 +81,17 @@ __device__ inline const T NT_CONST* constant(const T* p) {
 // count 0: a group without elements, whose record somebody has to write.
 #define NT_ROWS 0x80000000u
 struct Item {
-  uint32_t tensor, idx, slab, count;
+  uint32_t tensor, idx, group, count;
 };
 __device__ inline Item item_at(const Item* items, uint32_t i) {
   return __builtin_bit_cast(Item, ((const u32x4 NT_CONST*)(uintptr_t)items)[i]);
 }
-struct Slab {
-  uint32_t first, n, group, pad;   // items first .. first + n - 1
-};
+// A group's items are consecutive, and so are the partials (slots) that the blocks leave for it.  Block b of the norm's kernel walks items
+// b, b + blocks, ...: it meets a group whose items begin at item0 first at the item that is ((b - item0) mod blocks) further on, and
+// that number is its slot in the group.  A slab is a power of two of a group's slots.
 struct Group {
-  uint32_t first, n;               // slabs
-  int64_t elements;
+  uint32_t item0, slot0, slots, slab0;
+  int64_t elements, pad;
 };
 struct Shape {
   int64_t rows, cols;
@@ -72,16 +101,27 @@ struct Shape {
 // One way of cutting a list: items of one size, and what adds up their partials.
 struct Cut {
   const Item* items;
-  const Slab* slabs;
   const Group* groups;
   uint32_t* counters;   // of the slabs, then of the groups; zero before and after every launch
-  double* partials;     // one per item
+  double* partials;     // one per slot
   double* sums;         // one per slab
-  uint32_t nslabs;
+  uint32_t nitems, nslabs;
+  uint32_t blocks;      // a power of two
+  int shift;            // a slab is up to 1 << shift slots
 };
 struct Layout {
-  size_t shapes, items[2], slabs[2], groups[2], counters[2], upload, partials[2], sums[2], bytes;
+  size_t shapes, items[2], groups[2], counters[2], upload, partials[2], sums[2], bytes;
 };
+constexpr uint32_t BLOCKS[2] = {1u << 31, NT_LONG_BLOCKS};   // items of the first cut have a block each
+constexpr int64_t SIZES[2] = {NT_ITEM, NT_LONG_ITEM};
+// A slab is all slots, or about as many as there are slabs, so that neither counter is counted up often: a counter takes some 10 ns
+// per block, a second level some 3 us.
+int slab_shift(uint32_t slots) {
+  if (slots <= 128) return 7;
+  int shift = 4;
+  while (shift < 8 && slots >> (2 * shift)) ++shift;
+  return shift;
+}
 Layout layout_of(const nt_plan& p) {
   Layout l;
   size_t at = 0;
@@ -93,13 +133,12 @@ Layout layout_of(const nt_plan& p) {
   l.shapes = take(sizeof(Shape) * (size_t)p.tensors);
   for (int k = 0; k < 2; ++k) {
     l.items[k] = take(sizeof(Item) * (size_t)p.items[k]);
-    l.slabs[k] = take(sizeof(Slab) * (size_t)p.slabs[k]);
     l.groups[k] = take(p.items[k] ? sizeof(Group) * (size_t)p.groups : 0);
     l.counters[k] = take(p.items[k] ? 4 * NT_COUNTER_WORDS * ((size_t)p.slabs[k] + p.groups) : 0);
   }
   l.upload = at;
   for (int k = 0; k < 2; ++k) {
-    l.partials[k] = take(sizeof(double) * (size_t)p.items[k]);
+    l.partials[k] = take(sizeof(double) * (size_t)p.slots[k]);
     l.sums[k] = take(sizeof(double) * (size_t)p.slabs[k]);
   }
   l.bytes = at;
@@ -284,27 +323,29 @@ __device__ inline typename K::T total_of(const double* from, uint32_t n) {
   for (uint32_t i = threadIdx.x & 63; i < n; i += 64) t = K::join(t, __builtin_bit_cast(typename K::T, from[i]));
   return wave_total<K>(t);
 }
-// End of an item whose partial the block's lanes hold.
+// A block's part of group g, which its lanes hold: stored in its slot, counted, and added up by whoever comes last.  A block that meets
+// several groups alternates `half`, so that the first wave has read one half before another wave writes it again.
 template <class K, int THREADS>
-__device__ inline void end_item(const NormOut& o, uint32_t item, uint32_t slab_no, typename K::T acc) {
-  __shared__ typename K::T red[THREADS / 64];
+__device__ inline void end_part(const NormOut& o, uint32_t block, uint32_t g, typename K::T acc, int half = 0) {
+  __shared__ typename K::T red[2][THREADS / 64];
   acc = wave_total<K>(acc);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;
+  if ((threadIdx.x & 63) == 0) red[half][threadIdx.x >> 6] = acc;
   __syncthreads();
   if (threadIdx.x >= 64) return;
-  typename K::T total = red[0];
+  typename K::T total = red[half][0];
 #pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) total = K::join(total, red[w]);
-  const Slab NT_CONST* slab = constant(o.cut.slabs) + slab_no;
-  const uint32_t first = slab->first, n = slab->n, g = slab->group;
+  for (int w = 1; w < THREADS / 64; ++w) total = K::join(total, red[half][w]);
   const Group NT_CONST* group = constant(o.cut.groups) + g;
-  const uint32_t slab0 = group->first, slabs = group->n;
-  if (n > 1) {
-    if (!last_of(total, o.cut.partials + item, o.cut.counters + (size_t)NT_COUNTER_WORDS * slab_no, n)) return;
-    total = total_of<K>(o.cut.partials + first, n);
+  const uint32_t slot0 = group->slot0, slots = group->slots, slab0 = group->slab0;
+  const uint32_t slot = (block - group->item0) & (o.cut.blocks - 1), slab = slot >> o.cut.shift;
+  const uint32_t slabs = ((slots - 1) >> o.cut.shift) + 1, first = slab << o.cut.shift;
+  const uint32_t here = slots - first < (1u << o.cut.shift) ? slots - first : 1u << o.cut.shift;
+  if (here > 1) {
+    if (!last_of(total, o.cut.partials + slot0 + slot, o.cut.counters + (size_t)NT_COUNTER_WORDS * (slab0 + slab), here)) return;
+    total = total_of<K>(o.cut.partials + slot0 + first, here);
   }
   if (slabs > 1) {
-    if (!last_of(total, o.cut.sums + slab_no, o.cut.counters + (size_t)NT_COUNTER_WORDS * (o.cut.nslabs + g), slabs)) return;
+    if (!last_of(total, o.cut.sums + slab0 + slab, o.cut.counters + (size_t)NT_COUNTER_WORDS * (o.cut.nslabs + g), slabs)) return;
     total = total_of<K>(o.cut.sums + slab0, slabs);
   }
   if (threadIdx.x == 0) write_norm<K>(o, g, group->elements, total);
@@ -316,28 +357,167 @@ __device__ inline void end_item(const NormOut& o, uint32_t item, uint32_t slab_n
 struct ListArgs {
   const Shape* shapes;
   const Item* items;
-  const Slab* slabs;
   uint32_t item0;       // of this launch
 };
 
-template <class K>
-__global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_tensor* list, int level, uint32_t size, NormOut o) {
-  const uint32_t item = a.item0 + blockIdx.x;
-  const Item it = item_at(a.items, item);
-  typename K::T acc = 0;
-  if (it.count) {
-    const nt_tensor NT_CONST* t = constant(list) + it.tensor;
-    const int dtype = t->dtype;
-    for (uint32_t q = threadIdx.x; q < size / 4; q += NT_NORM_THREADS) {
-      const Spot s = spot(it, a.shapes, level, size, q);
-      if (s.n <= 0) continue;
-      const char NT_GLOBAL* p = address(t, dtype, s);
-      const f32x4 x = values(dtype, s.n == 4 ? load4(dtype, p) : load_part(dtype, p, s.n));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) K::add(acc, x[e]);   // the zeros of a part add nothing
+// Values of a type known at compile time, N of them in N * size bytes.
+template <int DTYPE, int N>
+struct Vec {
+  static constexpr int SIZE = DTYPE == NT_F32 ? 4 : 2, WORDS = N * SIZE / 4;
+  typedef uint32_t raw_t __attribute__((ext_vector_type(WORDS)));
+  typedef uint32_t any_t __attribute__((ext_vector_type(WORDS), aligned(SIZE)));
+  template <bool STREAM = false>
+  __device__ static inline raw_t load(const char NT_GLOBAL* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load((const any_t NT_GLOBAL*)p);
+    return *(const any_t NT_GLOBAL*)p;
+  }
+  template <bool STREAM = false>
+  __device__ static inline void store(char NT_GLOBAL* p, const raw_t& r) {
+    if constexpr (STREAM)
+      __builtin_nontemporal_store((any_t)r, (any_t NT_GLOBAL*)p);
+    else
+      *(any_t NT_GLOBAL*)p = r;
+  }
+  __device__ static inline float value(const raw_t& r, int e) {
+    if constexpr (DTYPE == NT_F32) return __builtin_bit_cast(float, (uint32_t)r[e]);
+    const uint32_t w = r[e >> 1];
+    if constexpr (DTYPE == NT_BF16) return __builtin_bit_cast(float, (e & 1) ? (w & 0xffff0000u) : (w << 16));
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)((e & 1) ? w >> 16 : w));
+  }
+  __device__ static inline void put(raw_t& r, int e, float x) {   // rounded to nearest even; elements in ascending order
+    if constexpr (DTYPE == NT_F32) {
+      r[e] = __builtin_bit_cast(uint32_t, x);
+    } else {
+      uint16_t h;
+      if constexpr (DTYPE == NT_BF16)
+        h = __builtin_bit_cast(uint16_t, (__bf16)x);
+      else
+        h = __builtin_bit_cast(uint16_t, (_Float16)x);
+      r[e >> 1] = (e & 1) ? (r[e >> 1] | (uint32_t)h << 16) : h;
     }
   }
-  end_item<K, NT_NORM_THREADS>(o, item, it.slab, acc);
+};
+template <int D>
+struct Dtype {
+  static constexpr int value = D;
+};
+// BODY(Dtype<the type>); the same for the whole block
+template <class BODY>
+__device__ inline void by_type(int dtype, BODY body) {
+  if (dtype == NT_F32)
+    body(Dtype<NT_F32>());
+  else if (dtype == NT_BF16)
+    body(Dtype<NT_BF16>());
+  else
+    body(Dtype<NT_F16>());
+}
+
+// n elements from p on, in 16-byte loads of which NT_NORM_FLIGHT are in flight; what is left over one by one.
+template <class K, int DTYPE, bool STREAM>
+__device__ inline void norm_flat(const char NT_GLOBAL* p, uint32_t n, typename K::T& total) {
+  constexpr int PER = DTYPE == NT_F32 ? 4 : 8, FLIGHT = NT_NORM_FLIGHT;
+  typedef Vec<DTYPE, PER> V;
+  typename K::T acc[2] = {total, 0};
+  auto take = [&](const typename V::raw_t& r) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) K::add(acc[e & 1], V::value(r, e));
+  };
+  const uint32_t whole = n / PER;
+  uint32_t i = threadIdx.x;
+  for (; i + (FLIGHT - 1) * NT_NORM_THREADS < whole; i += FLIGHT * NT_NORM_THREADS) {
+    typename V::raw_t r[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) r[k] = V::template load<STREAM>(p + 16 * (i + k * NT_NORM_THREADS));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) take(r[k]);
+  }
+  if (i < whole) {
+    typename V::raw_t r[FLIGHT - 1];
+#pragma unroll
+    for (int k = 0; k < FLIGHT - 1; ++k) {
+      r[k] = typename V::raw_t{};
+      if (i + k * NT_NORM_THREADS < whole) r[k] = V::template load<STREAM>(p + 16 * (i + k * NT_NORM_THREADS));
+    }
+#pragma unroll
+    for (int k = 0; k < FLIGHT - 1; ++k) take(r[k]);
+  }
+  if (threadIdx.x < n % PER) {
+    const uint32_t at = whole * PER + threadIdx.x;
+    if constexpr (DTYPE == NT_F32)
+      K::add(acc[0], __builtin_bit_cast(float, ((const uint32_t NT_GLOBAL*)p)[at]));
+    else
+      K::add(acc[0], Vec<DTYPE, 2>::value(typename Vec<DTYPE, 2>::raw_t{((const uint16_t NT_GLOBAL*)p)[at]}, 0));
+  }
+  total = K::join(acc[0], acc[1]);
+}
+// An item of a tensor with rows, four elements at a time.
+template <class K>
+__device__ inline void norm_rows(const nt_tensor NT_CONST* t, const Item& it, const Shape* shapes, int level, uint32_t size,
+                                 typename K::T& acc) {
+  constexpr int FLIGHT = 4;
+  const int dtype = t->dtype;
+  for (uint32_t q0 = threadIdx.x; q0 < size / 4; q0 += FLIGHT * NT_NORM_THREADS) {
+    u32x4 r[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      const uint32_t q = q0 + k * NT_NORM_THREADS;
+      const Spot s = spot(it, shapes, level, size, q);
+      const int n = q < size / 4 ? s.n : 0;
+      const char NT_GLOBAL* p = address(t, dtype, s);
+      if (n == 4)
+        r[k] = load4(dtype, p);
+      else
+        r[k] = load_part(dtype, p, n);
+    }
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+      const f32x4 x = values(dtype, r[k]);   // zeros, which add nothing, where there are no elements
+#pragma unroll
+      for (int e = 0; e < 4; ++e) K::add(acc, x[e]);
+    }
+  }
+}
+// A block walks every blocks-th item: the chip as a whole reads a long list from front to back, and neither the way to an item's address
+// nor the end of a part is met more often than need be.  The next item's record and address are fetched beside this one's elements.
+template <class K, bool STREAM>
+__global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_tensor* list, int level, NormOut o) {
+  const uint32_t size = level ? NT_LONG_ITEM : NT_ITEM;
+  uint32_t item = blockIdx.x;
+  Item it = item_at(a.items, item);
+  const nt_tensor NT_CONST* t = constant(list) + it.tensor;
+  const char NT_GLOBAL* data = nullptr;
+  int dtype = NT_F32, half = 0;
+  if (it.count) {
+    data = (const char NT_GLOBAL*)t->data;
+    dtype = t->dtype;
+  }
+  typename K::T acc = 0;
+  for (;;) {
+    const uint32_t next = item + o.cut.blocks;
+    const bool more = next < o.cut.nitems;
+    const Item nx = item_at(a.items, more ? next : item);
+    const nt_tensor NT_CONST* nt = constant(list) + nx.tensor;
+    const char NT_GLOBAL* const from = data + ((uint64_t)it.idx * size << size_shift(dtype));
+    const int type = dtype;
+    if (nx.count) {
+      data = (const char NT_GLOBAL*)nt->data;
+      dtype = nt->dtype;
+    }
+    if (it.count & NT_ROWS)
+      norm_rows<K>(t, it, a.shapes, level, size, acc);
+    else if (it.count)
+      by_type(type, [&](auto d) { norm_flat<K, decltype(d)::value, STREAM>(from, it.count, acc); });
+    if (!more || nx.group != it.group) {
+      end_part<K, NT_NORM_THREADS>(o, blockIdx.x, it.group, acc, half);
+      if (!more) return;
+      half ^= 1;
+      acc = 0;
+    }
+    item = next;
+    it = nx;
+    t = nt;
+  }
 }
 
 struct UpdateArgs {
@@ -348,52 +528,114 @@ struct UpdateArgs {
   float beta;
   int in_place;           // dst is src, and nothing is to be done where the factor is 1
 };
+// A whole item of a tensor of one row: all loads, then all stores.
+template <bool READ, class K, int XT, int YT, class ACC>
+__device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, float scale, float beta, ACC& acc) {
+  constexpr int PER = XT != NT_F32 && YT != NT_F32 ? 8 : 4, SWEEPS = NT_ITEM / (PER * NT_THREADS);
+  static_assert(SWEEPS * PER * NT_THREADS == NT_ITEM, "an item is whole sweeps");
+  typedef Vec<XT, PER> X;
+  typedef Vec<YT, PER> Y;
+  typename X::raw_t xr[SWEEPS];
+  typename Y::raw_t yr[SWEEPS];
+  const uint32_t lane = PER * threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    xr[k] = X::template load<UPD_NT_X>(x + X::SIZE * (lane + k * PER * NT_THREADS));
+    if constexpr (READ) yr[k] = Y::template load<UPD_NT_Y>(y + Y::SIZE * (lane + k * PER * NT_THREADS));
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    typename Y::raw_t z;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const float v = X::value(xr[k], e);
+      Y::put(z, e, READ ? __builtin_fmaf(scale, v, beta * Y::value(yr[k], e)) : scale * v);
+    }
+    Y::template store<UPD_NT_Y>(y + Y::SIZE * (lane + k * PER * NT_THREADS), z);
+    if constexpr (!__is_same(K, void)) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) K::add(acc, Y::value(z, e));
+    }
+  }
+}
+// Any item, four elements at a time.
+template <bool READ, class K, class ACC>
+__device__ inline void update_any(const nt_tensor NT_CONST* x, const nt_tensor NT_CONST* y, const Item& it, const Shape* shapes, float scale,
+                                  float beta, ACC& acc) {
+  constexpr int SWEEPS = NT_ITEM / (4 * NT_THREADS);
+  const int xt = x->dtype, yt = y->dtype;
+  Spot s[SWEEPS];
+  u32x4 xr[SWEEPS], yr[SWEEPS];
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    s[k] = spot(it, shapes, 0, NT_ITEM, threadIdx.x + k * NT_THREADS);
+    const char NT_GLOBAL* from = address(x, xt, s[k]);
+    const char NT_GLOBAL* to = address(y, yt, s[k]);
+    if (s[k].n == 4) {
+      xr[k] = load4(xt, from);
+      if constexpr (READ) yr[k] = load4(yt, to);
+    } else {
+      xr[k] = load_part(xt, from, s[k].n);
+      if constexpr (READ) yr[k] = load_part(yt, to, s[k].n);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    const f32x4 xv = values(xt, xr[k]);
+    f32x4 yv = {0.f, 0.f, 0.f, 0.f}, z;
+    if constexpr (READ) yv = values(yt, yr[k]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = READ ? __builtin_fmaf(scale, xv[e], beta * yv[e]) : scale * xv[e];
+    const u32x4 zr = rounded(yt, z);
+    char NT_GLOBAL* to = address(y, yt, s[k]);
+    if (s[k].n == 4)
+      store4(yt, to, zr);
+    else
+      store_part(yt, to, zr, s[k].n);
+    if constexpr (!__is_same(K, void)) {
+      const f32x4 v = values(yt, zr);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) K::add(acc, e < s[k].n ? v[e] : 0.f);
+    }
+  }
+}
+template <class K>
+struct Partial {
+  typedef typename K::T T;
+};
+template <>
+struct Partial<void> {
+  typedef int T;
+};
 // dst <- beta dst + scale factor src
 template <bool READ, class K>
 __global__ __launch_bounds__(NT_THREADS) void k_update(ListArgs a, UpdateArgs u, NormOut o) {
-  constexpr bool NORM = !__is_same(K, void);
   const uint32_t item = a.item0 + blockIdx.x;
   const Item it = item_at(a.items, item);
-  f32x4 stored = {0.f, 0.f, 0.f, 0.f};
+  typename Partial<K>::T acc = 0;
   if (it.count) {
     const nt_tensor NT_CONST* x = constant(u.src) + it.tensor;
     const nt_tensor NT_CONST* y = constant(u.dst) + it.tensor;
     float scale = (float)u.scale;
     if (u.norms) {
-      const float factor = (constant(u.norms) + (constant(a.slabs) + it.slab)->group)->factor;
+      const float factor = (constant(u.norms) + it.group)->factor;
       if (u.in_place && factor == 1.f) return;
       scale = (float)(u.scale * (double)factor);
     }
-    const Spot s = spot(it, a.shapes, 0, NT_ITEM, threadIdx.x);
-    if (s.n > 0) {
+    if (it.count == NT_ITEM) {
       const int xt = x->dtype, yt = y->dtype;
-      const char NT_GLOBAL* from = address(x, xt, s);
-      char NT_GLOBAL* to = address(y, yt, s);
-      const u32x4 xr = s.n == 4 ? load4(xt, from) : load_part(xt, from, s.n);
-      u32x4 yr = {0u, 0u, 0u, 0u};
-      if constexpr (READ) yr = s.n == 4 ? load4(yt, to) : load_part(yt, to, s.n);
-      const f32x4 xv = values(xt, xr), yv = values(yt, yr);
-      f32x4 z;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = READ ? __builtin_fmaf(scale, xv[e], u.beta * yv[e]) : scale * xv[e];
-      const u32x4 zr = rounded(yt, z);
-      if (s.n == 4)
-        store4(yt, to, zr);
-      else
-        store_part(yt, to, zr, s.n);
-      if constexpr (NORM) {
-        stored = values(yt, zr);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) stored[e] = e < s.n ? stored[e] : 0.f;   // inf * 0 of a part's end
-      }
+      const uint64_t at = (uint64_t)it.idx * NT_ITEM;
+      const char NT_GLOBAL* from = (const char NT_GLOBAL*)x->data + (at << size_shift(xt));
+      char NT_GLOBAL* to = (char NT_GLOBAL*)y->data + (at << size_shift(yt));
+      by_type(xt, [&](auto dx) {
+        by_type(yt, [&](auto dy) { update_flat<READ, K, decltype(dx)::value, decltype(dy)::value>(from, to, scale, u.beta, acc); });
+      });
+    } else {
+      update_any<READ, K>(x, y, it, a.shapes, scale, u.beta, acc);
     }
   }
-  if constexpr (NORM) {
-    typename K::T acc = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) K::add(acc, stored[e]);
-    end_item<K, NT_THREADS>(o, item, it.slab, acc);
-  }
+  if constexpr (!__is_same(K, void)) end_part<K, NT_THREADS>(o, item, it.group, acc);
 }
 
 struct AdamwArgs {
@@ -419,20 +661,45 @@ __device__ inline void adamw_element(const AdamwArgs& p, float g, float& w, floa
   const float upd = (p.step_size * m) * __builtin_amdgcn_rcpf(denom);
   w = __builtin_fmaf(p.decay, w, -upd);
 }
-__global__ __launch_bounds__(NT_THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
-  const Item it = item_at(a.items, a.item0 + blockIdx.x);
-  if (!it.count) return;
-  const nt_tensor NT_CONST* gt = constant(u.grads) + it.tensor;
-  const nt_tensor NT_CONST* wt = constant(u.w) + it.tensor;
-  const nt_tensor NT_CONST* mt = constant(u.m) + it.tensor;
-  const nt_tensor NT_CONST* vt = constant(u.v) + it.tensor;
-  float scale = (float)u.grad_scale;
-  if (u.norms) {
-    const nt_norm NT_CONST* n = constant(u.norms) + (constant(a.slabs) + it.slab)->group;
-    if ((u.flags & NT_SKIP_NONFINITE) && (n->status & NT_STATUS_NONFINITE)) return;
-    scale = (float)u.grad_scale * n->factor;
+// A whole item of a tensor of one row.
+template <int GT>
+__device__ inline void adamw_flat(const AdamwArgs& u, const char NT_GLOBAL* gp, char NT_GLOBAL* wp, char NT_GLOBAL* mp, char NT_GLOBAL* vp,
+                                  char NT_GLOBAL* cp, int copy_type, float scale) {
+  constexpr int SWEEPS = NT_ITEM / (4 * NT_ADAMW_THREADS);
+  typedef Vec<GT, 4> G;
+  typedef Vec<NT_F32, 4> F;
+  typename G::raw_t g[SWEEPS];
+  u32x4 w[SWEEPS], m[SWEEPS], v[SWEEPS];
+  const uint32_t lane = 4 * threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    const uint32_t at = lane + k * 4 * NT_ADAMW_THREADS;
+    g[k] = G::template load<ADAMW_NT_G>(gp + G::SIZE * at);
+    w[k] = F::template load<ADAMW_NT_S>(wp + 4 * at);
+    m[k] = F::template load<ADAMW_NT_S>(mp + 4 * at);
+    v[k] = F::template load<ADAMW_NT_S>(vp + 4 * at);
   }
-  const Spot s = spot(it, a.shapes, 0, NT_ITEM, threadIdx.x);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    const uint32_t at = lane + k * 4 * NT_ADAMW_THREADS;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float we = F::value(w[k], e), me = F::value(m[k], e), ve = F::value(v[k], e);
+      adamw_element(u, scale * G::value(g[k], e), we, me, ve);
+      F::put(w[k], e, we);
+      F::put(m[k], e, me);
+      F::put(v[k], e, ve);
+    }
+    F::template store<ADAMW_NT_S>(wp + 4 * at, w[k]);
+    F::template store<ADAMW_NT_S>(mp + 4 * at, m[k]);
+    F::template store<ADAMW_NT_S>(vp + 4 * at, v[k]);
+    if (cp) store4(copy_type, cp + (at << size_shift(copy_type)), rounded(copy_type, __builtin_bit_cast(f32x4, w[k])));
+  }
+}
+// Four elements, or the n of them that there are.
+__device__ inline void adamw_any(const AdamwArgs& u, const nt_tensor NT_CONST* gt, const nt_tensor NT_CONST* wt, const nt_tensor NT_CONST* mt,
+                                 const nt_tensor NT_CONST* vt, const nt_tensor NT_CONST* ct, const Spot& s, float scale) {
   if (s.n <= 0) return;
   const int dtype = gt->dtype;
   const char NT_GLOBAL* gp = address(gt, dtype, s);
@@ -459,26 +726,44 @@ __global__ __launch_bounds__(NT_THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
     m[e] = me;
     v[e] = ve;
   }
-  wr = __builtin_bit_cast(u32x4, w);
-  mr = __builtin_bit_cast(u32x4, m);
-  vr = __builtin_bit_cast(u32x4, v);
-  if (s.n == 4) {
-    store4(NT_F32, wp, wr);
-    store4(NT_F32, mp, mr);
-    store4(NT_F32, vp, vr);
-  } else {
-    store_part(NT_F32, wp, wr, s.n);
-    store_part(NT_F32, mp, mr, s.n);
-    store_part(NT_F32, vp, vr, s.n);
-  }
-  if (u.copy) {
-    const nt_tensor NT_CONST* ct = constant(u.copy) + it.tensor;
-    const int to = ct->dtype;
-    const u32x4 c = rounded(to, w);
+  auto put = [&](int type, char NT_GLOBAL* p, const u32x4& r) {
     if (s.n == 4)
-      store4(to, address(ct, to, s), c);
+      store4(type, p, r);
     else
-      store_part(to, address(ct, to, s), c, s.n);
+      store_part(type, p, r, s.n);
+  };
+  put(NT_F32, wp, __builtin_bit_cast(u32x4, w));
+  put(NT_F32, mp, __builtin_bit_cast(u32x4, m));
+  put(NT_F32, vp, __builtin_bit_cast(u32x4, v));
+  if (ct) put(ct->dtype, address(ct, ct->dtype, s), rounded(ct->dtype, w));
+}
+__global__ __launch_bounds__(NT_ADAMW_THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
+  const Item it = item_at(a.items, a.item0 + blockIdx.x);
+  if (!it.count) return;
+  const nt_tensor NT_CONST* gt = constant(u.grads) + it.tensor;
+  const nt_tensor NT_CONST* wt = constant(u.w) + it.tensor;
+  const nt_tensor NT_CONST* mt = constant(u.m) + it.tensor;
+  const nt_tensor NT_CONST* vt = constant(u.v) + it.tensor;
+  const nt_tensor NT_CONST* ct = u.copy ? constant(u.copy) + it.tensor : nullptr;
+  float scale = (float)u.grad_scale;
+  if (u.norms) {
+    const nt_norm NT_CONST* n = constant(u.norms) + it.group;
+    if ((u.flags & NT_SKIP_NONFINITE) && (n->status & NT_STATUS_NONFINITE)) return;
+    scale = (float)u.grad_scale * n->factor;
+  }
+  if (it.count == NT_ITEM) {
+    const uint64_t at = (uint64_t)it.idx * NT_ITEM;
+    const int dtype = gt->dtype, copy_type = ct ? ct->dtype : 0;
+    const char NT_GLOBAL* gp = (const char NT_GLOBAL*)gt->data + (at << size_shift(dtype));
+    char NT_GLOBAL* cp = ct ? (char NT_GLOBAL*)ct->data + (at << size_shift(copy_type)) : nullptr;
+    by_type(dtype, [&](auto d) {
+      adamw_flat<decltype(d)::value>(u, gp, (char NT_GLOBAL*)wt->data + 4 * at, (char NT_GLOBAL*)mt->data + 4 * at,
+                                     (char NT_GLOBAL*)vt->data + 4 * at, cp, copy_type, scale);
+    });
+  } else {
+#pragma unroll 1
+    for (uint32_t q = threadIdx.x; q < NT_ITEM / 4; q += NT_ADAMW_THREADS)
+      adamw_any(u, gt, wt, mt, vt, ct, spot(it, a.shapes, 0, NT_ITEM, q), scale);
   }
 }
 
@@ -501,17 +786,10 @@ Pieces pieces_of(int64_t rows, int64_t cols, int64_t size) {
   const int64_t per_item = (size / 4) / ceil_div(cols, 4);
   return {ceil_div(rows, per_item), 0, (uint32_t)per_item};
 }
-// Items of a slab: about as many as there are slabs, so that neither count is long.
-uint32_t slab_items(int64_t items) {
-  uint32_t n = 16;
-  while (n < 256 && (int64_t)n * n < items) n *= 2;
-  return n;
-}
-
 Cut cut_of(const nt_plan& p, const Layout& l, int k) {
   char* const b = (char*)p.image;
-  return {(const Item*)(b + l.items[k]), (const Slab*)(b + l.slabs[k]), (const Group*)(b + l.groups[k]), (uint32_t*)(b + l.counters[k]),
-          (double*)(b + l.partials[k]), (double*)(b + l.sums[k]), p.slabs[k]};
+  return {(const Item*)(b + l.items[k]), (const Group*)(b + l.groups[k]), (uint32_t*)(b + l.counters[k]), (double*)(b + l.partials[k]),
+          (double*)(b + l.sums[k]), p.items[k], p.slabs[k], BLOCKS[k], slab_shift(p.slots[k])};
 }
 
 int check_plan(const nt_plan* p) {
@@ -542,7 +820,7 @@ int in_launches(uint32_t items, uint32_t most, LAUNCH launch) {
 template <bool READ>
 int enqueue_update(const nt_plan& p, const Layout& l, const UpdateArgs& u, int kind, const NormOut& o, hipStream_t st) {
   const Cut cut = cut_of(p, l, 0);
-  ListArgs a = {(const Shape*)((char*)p.image + l.shapes), cut.items, cut.slabs, 0};
+  ListArgs a = {(const Shape*)((char*)p.image + l.shapes), cut.items, 0};
   return in_launches(p.items[0], NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
     if (!o.norms)
@@ -576,7 +854,6 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
   p.groups = G;
   p.magic = NT_PLAN_MAGIC;
   const int cuts = elements >= NT_LONG_LIST ? 2 : 1;
-  const int64_t sizes[2] = {NT_ITEM, NT_LONG_ITEM};
 
   // the tensors in the order of their groups; a group without items gets an empty one
   int64_t* const first = new (std::nothrow) int64_t[(size_t)G + 1]();
@@ -596,26 +873,24 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
   // first[g] is now the end of group g
   auto group_begin = [&](int32_t g) { return g ? first[g - 1] : 0; };
 
-  uint32_t per_slab[2] = {0, 0};
+  auto items_of = [&](int32_t g, int k) {   // at least the empty one
+    int64_t n = 0;
+    for (int64_t j = group_begin(g); j < first[g]; ++j) n += pieces_of(tensors[order[j]].rows, tensors[order[j]].cols, SIZES[k]).n;
+    return n ? n : 1;
+  };
+  auto slots_of = [](int64_t items, int k) { return items < BLOCKS[k] ? items : (int64_t)BLOCKS[k]; };
   for (int k = 0; k < cuts; ++k) {
-    int64_t items = 0;
-    for (int32_t i = 0; i < N; ++i) {
-      items += pieces_of(tensors[i].rows, tensors[i].cols, sizes[k]).n;
+    int64_t items = 0, slots = 0, slabs = 0;
+    for (int32_t g = 0; g < G; ++g) {
+      const int64_t here = items_of(g, k);
+      items += here;
+      slots += slots_of(here, k);
       if (items > (1ll << 31) - 1) return NT_ERR_TOO_LARGE;
     }
-    per_slab[k] = slab_items(items);
-    int64_t slabs = 0;
-    for (int32_t g = 0; g < G; ++g) {
-      int64_t here = 0;
-      for (int64_t j = group_begin(g); j < first[g]; ++j) here += pieces_of(tensors[order[j]].rows, tensors[order[j]].cols, sizes[k]).n;
-      if (here == 0) {
-        ++items;
-        here = 1;
-      }
-      slabs += ceil_div(here, per_slab[k]);
-    }
-    if (items > (1ll << 31) - 1) return NT_ERR_TOO_LARGE;
+    const int shift = slab_shift((uint32_t)slots);
+    for (int32_t g = 0; g < G; ++g) slabs += ceil_div(slots_of(items_of(g, k), k), 1ll << shift);
     p.items[k] = (uint32_t)items;
+    p.slots[k] = (uint32_t)slots;
     p.slabs[k] = (uint32_t)slabs;
   }
   const Layout l = layout_of(p);
@@ -630,42 +905,37 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
       s.rows = tensors[i].rows;
       s.cols = tensors[i].cols;
       for (int k = 0; k < cuts; ++k) {
-        const Pieces c = pieces_of(s.rows, s.cols, sizes[k]);
+        const Pieces c = pieces_of(s.rows, s.cols, SIZES[k]);
         s.per_row[k] = c.per_row;
         s.rows_per_item[k] = c.rows_per_item;
       }
     }
     for (int k = 0; k < cuts; ++k) {
-      Item* items = (Item*)(b + l.items[k]);
-      Slab* slabs = (Slab*)(b + l.slabs[k]);
-      Group* groups = (Group*)(b + l.groups[k]);
-      uint32_t item = 0, slab = 0;
+      Item* const items = (Item*)(b + l.items[k]);
+      Group* const groups = (Group*)(b + l.groups[k]);
+      const int shift = slab_shift(p.slots[k]);
+      uint32_t item = 0, slot = 0, slab = 0;
       for (int32_t g = 0; g < G; ++g) {
-        groups[g].first = slab;
         const uint32_t begin = item;
-        auto put = [&](uint32_t tensor, uint32_t idx, uint32_t count) {
-          const uint32_t in = (item - begin) % per_slab[k];
-          if (in == 0) slabs[slab++] = {item, 0, (uint32_t)g, 0};
-          slabs[slab - 1].n = in + 1;
-          items[item++] = {tensor, idx, slab - 1, count};
-        };
+        int64_t held_elements = 0;
         for (int64_t j = group_begin(g); j < first[g]; ++j) {
           const nt_tensor& t = tensors[order[j]];
-          groups[g].elements += t.rows * t.cols;
-          const Pieces c = pieces_of(t.rows, t.cols, sizes[k]);
+          held_elements += t.rows * t.cols;
+          const Pieces c = pieces_of(t.rows, t.cols, SIZES[k]);
           for (int64_t idx = 0; idx < c.n; ++idx) {
-            int64_t count;
+            int64_t count = 1;   // of a part of a row
             if (t.rows == 1)
-              count = t.cols - idx * sizes[k] < sizes[k] ? t.cols - idx * sizes[k] : sizes[k];
-            else if (c.per_row)
-              count = 1 | (int64_t)NT_ROWS;
-            else
-              count = (t.rows - idx * c.rows_per_item < c.rows_per_item ? t.rows - idx * c.rows_per_item : c.rows_per_item) | (int64_t)NT_ROWS;
-            put((uint32_t)order[j], (uint32_t)idx, (uint32_t)count);
+              count = t.cols - idx * SIZES[k] < SIZES[k] ? t.cols - idx * SIZES[k] : SIZES[k];
+            else if (!c.per_row)
+              count = t.rows - idx * c.rows_per_item < c.rows_per_item ? t.rows - idx * c.rows_per_item : c.rows_per_item;
+            items[item++] = {(uint32_t)order[j], (uint32_t)idx, (uint32_t)g, (uint32_t)count | (t.rows == 1 ? 0u : NT_ROWS)};
           }
         }
-        if (item == begin) put(0, 0, 0);
-        groups[g].n = slab - groups[g].first;
+        if (item == begin) items[item++] = {0, 0, (uint32_t)g, 0};
+        const uint32_t slots = (uint32_t)slots_of(item - begin, k);
+        groups[g] = {begin, slot, slots, slab, held_elements, 0};
+        slot += slots;
+        slab += (uint32_t)ceil_div(slots, 1ll << shift);
       }
     }
   }
@@ -694,17 +964,16 @@ int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind
   if (rc != NT_OK) return rc;
   const Layout l = layout_of(*plan);
   const int k = plan->items[1] ? 1 : 0;
-  const uint32_t size = k ? NT_LONG_ITEM : NT_ITEM;
   const NormOut o = {cut_of(*plan, l, k), max_norm, grad_scale, norms};
-  ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), o.cut.items, o.cut.slabs, 0};
-  hipStream_t st = (hipStream_t)hip_stream;
-  return in_launches(plan->items[k], NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
-    a.item0 = at;
-    if (kind == NT_NORM_L2)
-      hipLaunchKernelGGL(k_norm<Square>, dim3(n), dim3(NT_NORM_THREADS), 0, st, a, grads, k, size, o);
-    else
-      hipLaunchKernelGGL(k_norm<Largest>, dim3(n), dim3(NT_NORM_THREADS), 0, st, a, grads, k, size, o);
-  });
+  const ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), o.cut.items, 0};
+  const uint32_t blocks = o.cut.nitems < o.cut.blocks ? o.cut.nitems : o.cut.blocks;
+  const bool stream = plan->elements >= NT_STREAM_NORM;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT_NORM_THREADS), 0, (hipStream_t)hip_stream, a, grads, k, o);
+    return hip_code(hipGetLastError());
+  };
+  if (kind == NT_NORM_L2) return stream ? launch(k_norm<Square, true>) : launch(k_norm<Square, false>);
+  return stream ? launch(k_norm<Largest, true>) : launch(k_norm<Largest, false>);
 }
 
 int normtest_clip_grads(const nt_plan* plan, const nt_tensor* grads, const nt_tensor* out, const nt_norm* norms, void* hip_stream) {
@@ -757,11 +1026,11 @@ int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt
                        (float)hyper->eps};
   const Layout l = layout_of(*plan);
   const Cut cut = cut_of(*plan, l, 0);
-  ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), cut.items, cut.slabs, 0};
+  ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), cut.items, 0};
   hipStream_t st = (hipStream_t)hip_stream;
-  return in_launches(plan->items[0], NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
+  return in_launches(plan->items[0], NT_ADAMW_LAUNCH, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
-    hipLaunchKernelGGL(k_adamw, dim3(n), dim3(NT_THREADS), 0, st, a, u);
+    hipLaunchKernelGGL(k_adamw, dim3(n), dim3(NT_ADAMW_THREADS), NT_ADAMW_LDS, st, a, u);
   });
 }
 

@@ -25,8 +25,15 @@ def plan_of(shapes, groups=None, G=None):
     return plan, image
 
 
+def slab_shift(slots):
+    shift = 4
+    while shift < 8 and slots >> (2 * shift):
+        shift += 1
+    return 7 if slots <= 128 else shift
+
+
 def cuts_of(plan, image):
-    """The image's parts: per cut (items, slabs, groups, counters) as arrays, and the shapes."""
+    """The image's parts: per cut (items, groups, counters) as arrays, and the shapes."""
     at = 0
 
     def take(n, dtype):
@@ -39,13 +46,15 @@ def cuts_of(plan, image):
     cuts = []
     for k in range(2):
         here = plan.items[k] > 0
-        items = take(plan.items[k], np.dtype([("tensor", "u4"), ("idx", "u4"), ("slab", "u4"), ("count", "u4")]))
-        slabs = take(plan.slabs[k], np.dtype([("first", "u4"), ("n", "u4"), ("group", "u4"), ("pad", "u4")]))
-        groups = take(plan.groups if here else 0, np.dtype([("first", "u4"), ("n", "u4"), ("elements", "i8")]))
+        items = take(plan.items[k], np.dtype([("tensor", "u4"), ("idx", "u4"), ("group", "u4"), ("count", "u4")]))
+        groups = take(plan.groups if here else 0, np.dtype([("item0", "u4"), ("slot0", "u4"), ("slots", "u4"), ("slab0", "u4"),
+                                                            ("elements", "i8"), ("pad", "i8")]))
         counters = take(16 * (plan.slabs[k] + plan.groups) if here else 0, "u4")
         if here:
-            cuts.append((items, slabs, groups, counters))
+            cuts.append((items, groups, counters))
     assert at == plan.upload_bytes
+    scratch = sum((8 * n + 63) // 64 * 64 for n in (*plan.slots, *plan.slabs))
+    assert plan.bytes == plan.upload_bytes + scratch
     return shapes, cuts
 
 
@@ -85,8 +94,8 @@ def test_every_element_is_in_one_item(shapes, long_list):
     plan, image = plan_of(shapes)
     held, cuts = cuts_of(plan, image)
     assert len(cuts) == (2 if long_list else 1) and plan.elements == sum(r * c for r, c in shapes)
-    for k, (items, slabs, groups, counters) in enumerate(cuts):
-        size = [ITEM, 32768][k]
+    for k, (items, groups, counters) in enumerate(cuts):
+        size = [ITEM, 8192][k]
         seen = [np.zeros((r, c), np.int32) if r * c < 1 << 20 else None for r, c in shapes]
         for item in items:
             if item["count"] and seen[item["tensor"]] is not None:
@@ -99,23 +108,39 @@ def test_every_element_is_in_one_item(shapes, long_list):
         assert not counters.any()
 
 
-@pytest.mark.parametrize("seed", range(6))
-def test_slabs_and_groups_partition_the_items(seed):
+@pytest.mark.parametrize("seed", range(12))
+def test_slots_and_slabs_are_a_groups_own(seed):
+    """The blocks' walk over the items as the kernels make it: every part that a block leaves has a slot of its own inside its group's, and
+    the counters of slabs and groups are counted up as often as the last block expects."""
     rng = random.Random(seed)
     shapes = [rng.choice([(1, 0), (1, rng.randrange(1, 40000)), (rng.randrange(2, 300), rng.randrange(1, 900))]) for _ in range(rng.choice([1, 40, 300]))]
+    if seed % 2:
+        shapes += [(1, rng.randrange(1 << 23, 1 << 25)), (1 << 12, rng.randrange(100, 9000))]
     G = rng.choice([1, 3, 50])
     groups = [rng.randrange(G) for _ in shapes]
     plan, image = plan_of(shapes, groups, G)
     _, cuts = cuts_of(plan, image)
-    for items, slabs, grps, _ in cuts:
-        assert (items["slab"] == np.repeat(np.arange(len(slabs)), slabs["n"])).all()
-        assert (slabs["first"] == np.cumsum(slabs["n"]) - slabs["n"]).all() and (slabs["n"] <= 256).all()
-        assert (slabs["group"] == np.repeat(np.arange(G), grps["n"])).all() and (grps["n"] > 0).all()
+    assert len(cuts) == (2 if plan.elements >= 1 << 23 else 1)
+    for k, (items, grps, _) in enumerate(cuts):
+        blocks = [1 << 31, 1024][k]
+        shift = slab_shift(plan.slots[k])
+        assert (np.diff(items["group"].astype(np.int64)) >= 0).all() and set(items["group"]) == set(range(G))
+        parts = {}   # group -> slots in the order of their blocks
+        for b in range(min(blocks, len(items))):
+            mine = items["group"][b::blocks] if blocks < len(items) else items["group"][b:b + 1]
+            for g in np.unique(mine):
+                parts.setdefault(int(g), []).append((b - int(grps["item0"][g])) % blocks)
+        slot0 = slab0 = 0
         for g in range(G):
             assert grps["elements"][g] == sum(r * c for (r, c), h in zip(shapes, groups) if h == g)
+            assert (int(grps["slot0"][g]), int(grps["slab0"][g])) == (slot0, slab0)
+            assert sorted(parts[g]) == list(range(grps["slots"][g]))
+            slot0 += int(grps["slots"][g])
+            slab0 += ((int(grps["slots"][g]) - 1) >> shift) + 1
+        assert (slot0, slab0) == (plan.slots[k], plan.slabs[k])
         for item in items:
             if item["count"]:
-                assert groups[item["tensor"]] == slabs["group"][item["slab"]]
+                assert groups[item["tensor"]] == item["group"]
 
 
 def test_sizes_that_a_plan_refuses():
@@ -186,7 +211,7 @@ def test_calls_refuse_bad_arguments_before_any_launch():
 
 
 def test_records_have_the_headers_layout():
-    assert ctypes.sizeof(B.nt_tensor) == 40 and ctypes.sizeof(B.nt_norm) == B.NORM_BYTES == 40 and ctypes.sizeof(B.nt_plan) == 64
+    assert ctypes.sizeof(B.nt_tensor) == 40 and ctypes.sizeof(B.nt_norm) == B.NORM_BYTES == 40 and ctypes.sizeof(B.nt_plan) == 72
     raw = struct.pack("ddffIiq", 3.0, 0.5, 3.0, 0.25, 1, 1, 7)
     norms = torch.frombuffer(bytearray(raw * 2), dtype=torch.uint8)
     assert [r.as_dict() for r in B.read_norms(norms)] == [dict(norm=3.0, coef=0.5, norm32=3.0, factor=0.25, status=1, clipped=1, elements=7)] * 2
