@@ -194,7 +194,8 @@ def lib(path: Optional[str] = None):
         L.normtest_strerror.argtypes = [ctypes.c_int]
         L.normtest_strerror.restype = ctypes.c_char_p
         for name in ("normtest_step", "normtest_step_rows", "normtest_step_clipped", "normtest_adamw_gbar", "normtest_layer_stats",
-                     "normtest_workspace_bytes_for"):
+                     "normtest_workspace_bytes_for", "normtest_grad_norm", "normtest_clip_grads", "normtest_accumulate",
+                     "normtest_adamw_tensors"):
             setattr(L, name + "_entry", ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
         if _lib is None:
             _fast = _load_callpath()
@@ -551,6 +552,9 @@ class TensorList:
         self.table.copy_(host)
         self.addresses = [t.data_ptr() for t in self.tensors]
         self.dtypes = {t.dtype for t in self.tensors}
+        # for the native call path; None: its calls are then left to Python
+        self.native = _fast and _fast.make_list(self.tensors, self.addresses, ctypes.addressof(self.plan.record), self.plan.record, self.table,
+                                                self.plan.stream)
 
     def refresh(self, tensors=None) -> "TensorList":
         """Reads the tensors' addresses again, or those of other tensors of the same shapes and layouts (gradients that were allocated
@@ -677,6 +681,13 @@ def _list_call(where: str, plan: TensorPlan, lists, norms, stream, fn, *args):
             lst.table.record_stream(stream)
 
 
+def _native(lst):
+    """What the native call path knows a list by: None for no list, False for what it does not take."""
+    if lst is None:
+        return None
+    return (lst.native or False) if type(lst) is TensorList else False
+
+
 def _first(where: str, lst) -> TensorPlan:
     if not isinstance(lst, TensorList):
         raise TypeError("%s takes lists made by make_tensor_list, got %s" % (where, type(lst).__name__))
@@ -687,6 +698,9 @@ def normtest_grad_norm(grads: TensorList, norms: Optional[torch.Tensor] = None, 
                        kind: int = NT_NORM_L2, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Enqueue the norms of the list's groups and their clipping factors for max_norm (0: none) on `stream` (default: torch's current
     stream).  Returns the device memory of the records (norms, or new): read_norms after a sync, norm_views without one."""
+    if stream is None and norms is not None and type(grads) is TensorList:
+        if _fast and _done(_fast.grad_norm(_lib.normtest_grad_norm_entry, grads.native, kind, max_norm, grad_scale, norms), "normtest_grad_norm"):
+            return norms
     plan = _first("normtest_grad_norm", grads)
     if norms is None:
         norms = make_norms(grads)
@@ -698,6 +712,9 @@ def normtest_grad_norm(grads: TensorList, norms: Optional[torch.Tensor] = None, 
 def normtest_clip_grads(grads: TensorList, norms: torch.Tensor, *, out: Optional[TensorList] = None,
                         stream: Optional[torch.cuda.Stream] = None) -> None:
     """Multiply the gradients by their groups' factors, in place or into the list `out` (of any types)."""
+    if stream is None and type(grads) is TensorList:
+        if _fast and _done(_fast.clip_grads(_lib.normtest_clip_grads_entry, grads.native, _native(out), norms), "normtest_clip_grads"):
+            return
     plan = _first("normtest_clip_grads", grads)
     _list_call("normtest_clip_grads", plan, (grads,) if out is None else (grads, out), (norms,), stream, lib().normtest_clip_grads,
                grads.table.data_ptr(), None if out is None else out.table.data_ptr(), norms.data_ptr())
@@ -718,6 +735,10 @@ def normtest_accumulate(dst: TensorList, src: TensorList, *, beta: float = 1.0, 
     """dst <- beta dst + scale src, in fp32, rounded once to dst's types (beta 0: dst is not read).  src_norms: records whose factors
     multiply src too (every micro-batch clipped by itself).  norms: records that receive the norms of what is stored, as
     normtest_grad_norm(dst) with max_norm, grad_scale and kind would, from the same pass."""
+    if stream is None and type(dst) is TensorList:
+        if _fast and _done(_fast.accumulate(_lib.normtest_accumulate_entry, dst.native, _native(src), beta, scale, src_norms, kind, max_norm,
+                                            grad_scale, norms), "normtest_accumulate"):
+            return
     plan = _first("normtest_accumulate", dst)
     _list_call("normtest_accumulate", plan, (dst, src), (src_norms, norms), stream, lib().normtest_accumulate, dst.table.data_ptr(),
                src.table.data_ptr() if isinstance(src, TensorList) else None, float(beta), float(scale), _ptr(src_norms), kind, float(max_norm),
@@ -731,6 +752,10 @@ def normtest_adamw_tensors(grads: TensorList, w: TensorList, m: TensorList, v: T
     lists w, m, v; copy: a list of any types that receives the new weights.  skip_nonfinite: tensors of a group whose norm is not finite
     are left alone."""
     where = "normtest_adamw_tensors"
+    if stream is None and type(grads) is TensorList:
+        if _fast and _done(_fast.adamw_tensors(_lib.normtest_adamw_tensors_entry, grads.native, _native(w), _native(m), _native(v), _native(copy),
+                                               hyper, grad_scale, norms, NT_SKIP_NONFINITE if skip_nonfinite else 0), where):
+            return
     plan = _first(where, grads)
     lists = (grads, w, m, v) if copy is None else (grads, w, m, v, copy)
     for lst in lists[1:4]:

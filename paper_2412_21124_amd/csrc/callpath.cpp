@@ -12,6 +12,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <memory>
+#include <vector>
 
 #include "normtest.h"
 
@@ -256,6 +258,142 @@ PyObject* layer_stats(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- lists of tensors ----
+// A list as the binding made it: its tensors with the addresses that its table on the device holds, and its plan.
+struct List {
+  std::vector<at::Tensor> tensors;
+  std::vector<const void*> addresses;
+  const nt_plan* plan;
+  const nt_tensor* table;
+  c10::Device device = c10::Device(c10::DeviceType::CPU);
+  void* stream;      // that the tables were made on: another one has to hold their memory, which is left to Python
+  bool all_f32;
+  PyObject* owner;   // of the plan's record
+};
+const char list_name[] = "normtest.list";
+void list_free(PyObject* capsule) {
+  List* l = (List*)PyCapsule_GetPointer(capsule, list_name);
+  if (!l) return;
+  Py_XDECREF(l->owner);
+  delete l;
+}
+// make_list(tensors, addresses, plan's address, its owner, table, stream's handle); tensors: a tuple, addresses: a list
+PyObject* make_list(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    if (!PyTuple_CheckExact(a[0]) || !PyList_CheckExact(a[1]) || PyTuple_GET_SIZE(a[0]) != PyList_GET_SIZE(a[1])) throw Refused();
+    std::unique_ptr<List> l(new List());
+    l->all_f32 = true;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
+      l->tensors.push_back(tensor(PyTuple_GET_ITEM(a[0], i)));
+      l->addresses.push_back(PyLong_AsVoidPtr(PyList_GET_ITEM(a[1], i)));
+      if (!l->addresses.back() && PyErr_Occurred()) throw Refused();
+      l->all_f32 = l->all_f32 && l->tensors.back().scalar_type() == at::kFloat;
+    }
+    l->plan = entry<const nt_plan>(a[2]);
+    const at::Tensor& table = tensor(a[4]);
+    l->table = (const nt_tensor*)table.data_ptr();
+    l->device = table.device();
+    l->stream = PyLong_AsVoidPtr(a[5]);
+    if (!l->stream && PyErr_Occurred()) throw Refused();
+    PyObject* capsule = PyCapsule_New(l.get(), list_name, list_free);
+    if (!capsule) throw Refused();
+    Py_INCREF(a[3]);
+    l->owner = a[3];
+    l.release();
+    return capsule;
+  });
+}
+// The list behind a capsule, its tensors where its table says; `first`: the list whose plan it has to share.
+const List* list_of(PyObject* o, const List* first) {
+  if (!PyCapsule_IsValid(o, list_name)) throw Refused();
+  const List* l = (const List*)PyCapsule_GetPointer(o, list_name);
+  if (first && l->plan != first->plan) throw Refused();
+  for (size_t i = 0; i < l->tensors.size(); ++i)
+    if (l->tensors[i].data_ptr() != l->addresses[i]) throw Refused();
+  return l;
+}
+const List* list_or_none(PyObject* o, const List* first) { return o == Py_None ? nullptr : list_of(o, first); }
+nt_norm* norms_of(PyObject* o, const List& l, bool required) {
+  if (o == Py_None && !required) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.device() != l.device || !t.is_contiguous() || (size_t)(t.numel() * t.element_size()) < (size_t)l.plan->groups * sizeof(nt_norm))
+    throw Refused();
+  return (nt_norm*)t.data_ptr();
+}
+// The current stream, if it is the one the tables were made on and its device the current one.
+void* stream_of_list(const List& l) {
+  if (c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != l.device) throw Refused();
+  void* st = stream_of(l.device);
+  if (st != l.stream) throw Refused();
+  return st;
+}
+double number(PyObject* o) {
+  if (!PyFloat_CheckExact(o)) throw Refused();
+  return PyFloat_AS_DOUBLE(o);
+}
+int32_t small(PyObject* o) {
+  const int64_t x = integer(o);
+  if (x < 0 || x > 1 << 16) throw Refused();
+  return (int32_t)x;
+}
+
+// grad_norm(entry, grads, kind, max_norm, grad_scale, norms)
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&] {
+    auto* f = entry<decltype(normtest_grad_norm)>(a[0]);
+    const List& g = *list_of(a[1], nullptr);
+    const int32_t kind = small(a[2]);
+    const double max_norm = number(a[3]), scale = number(a[4]);
+    nt_norm* norms = norms_of(a[5], g, true);
+    void* st = stream_of_list(g);
+    return enqueue([&] { return f(g.plan, g.table, kind, max_norm, scale, norms, st); });
+  });
+}
+
+// clip_grads(entry, grads, out, norms)
+PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&] {
+    auto* f = entry<decltype(normtest_clip_grads)>(a[0]);
+    const List& g = *list_of(a[1], nullptr);
+    const List* out = list_or_none(a[2], &g);
+    const nt_norm* norms = norms_of(a[3], g, true);
+    void* st = stream_of_list(g);
+    return enqueue([&] { return f(g.plan, g.table, out ? out->table : nullptr, norms, st); });
+  });
+}
+
+// accumulate(entry, dst, src, beta, scale, src_norms, kind, max_norm, grad_scale, norms)
+PyObject* accumulate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    auto* f = entry<decltype(normtest_accumulate)>(a[0]);
+    const List& dst = *list_of(a[1], nullptr);
+    const List& src = *list_of(a[2], &dst);
+    const double beta = number(a[3]), scale = number(a[4]), max_norm = number(a[7]), grad_scale = number(a[8]);
+    const nt_norm* src_norms = norms_of(a[5], dst, false);
+    const int32_t kind = small(a[6]);
+    nt_norm* norms = norms_of(a[9], dst, false);
+    void* st = stream_of_list(dst);
+    return enqueue([&] { return f(dst.plan, dst.table, src.table, beta, scale, src_norms, kind, max_norm, grad_scale, norms, st); });
+  });
+}
+
+// adamw_tensors(entry, grads, w, m, v, copy, hyper, grad_scale, norms, flags)
+PyObject* adamw_tensors(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    auto* f = entry<decltype(normtest_adamw_tensors)>(a[0]);
+    const List& g = *list_of(a[1], nullptr);
+    const List &w = *list_of(a[2], &g), &m = *list_of(a[3], &g), &v = *list_of(a[4], &g);
+    if (!w.all_f32 || !m.all_f32 || !v.all_f32) throw Refused();
+    const List* copy = list_or_none(a[5], &g);
+    const nt_hyper* hyper = structure<nt_hyper>(a[6], hyper_type);
+    const double scale = number(a[7]);
+    const nt_norm* norms = norms_of(a[8], g, false);
+    const int32_t flags = small(a[9]);
+    void* st = stream_of_list(g);
+    return enqueue([&] { return f(g.plan, g.table, w.table, m.table, v.table, copy ? copy->table : nullptr, hyper, scale, norms, (uint32_t)flags, st); });
+  });
+}
+
 // init(nt_hyper, nt_shard_info, torch.nn.Parameter, torch._C._cuda_getCurrentRawStream)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 4, [&]() -> PyObject* {
@@ -270,7 +408,8 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init),       FAST(step),        FAST(step_clipped), FAST(step_rows),
-                         FAST(adamw_gbar), FAST(layer_stats), {nullptr, nullptr, 0, nullptr}};
+                         FAST(adamw_gbar), FAST(layer_stats), FAST(make_list), FAST(grad_norm), FAST(clip_grads), FAST(accumulate),
+                         FAST(adamw_tensors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_callpath", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

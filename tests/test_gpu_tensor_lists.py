@@ -353,6 +353,76 @@ def test_the_same_bits_again_and_counters_back_at_zero():
     assert torch.equal(lst.plan.image[:lst.plan.record.upload_bytes], image)
 
 
+class Recorded:
+    """The native call path, and what it has returned: None for a call that it left to Python."""
+    def __init__(self, fast):
+        self.fast, self.back = fast, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.back.append(getattr(self.fast, name)(*args))
+            return self.back[-1]
+        return call
+
+
+class Other(torch.Tensor):
+    pass
+
+
+def test_the_native_call_path_and_the_checks_in_python_agree(monkeypatch):
+    shapes = [(5000,), (3, 700), (0,)]
+    fast = Recorded(B._fast)
+    results = []
+    for path in (fast, None):
+        monkeypatch.setattr(B, "_fast", path)
+        x, _ = carve(shapes, [BF16, F32, F16], 50, extra=2)
+        (w, m, v), _ = state(shapes)
+        c, _ = carve(shapes, [BF16] * 3, 51)
+        g = B.make_tensor_list(x, groups=[0, 1, 0])
+        lists = [B.make_tensor_list(t, like=g) for t in (w, m, v, c)]
+        norms, after = B.make_norms(g), B.make_norms(g)
+        fast.back = []
+        B.normtest_grad_norm(g, norms, max_norm=0.5, kind=B.NT_NORM_MAX)
+        B.normtest_grad_norm(g, norms, max_norm=0.5)
+        B.normtest_adamw_tensors(g, *lists[:3], hyper(), norms=norms, copy=lists[3], skip_nonfinite=True)
+        B.normtest_adamw_tensors(g, *lists[:3], hyper(), grad_scale=0.5)
+        B.normtest_accumulate(lists[0], g, src_norms=norms, norms=after, beta=0.5)
+        B.normtest_accumulate(lists[1], g, beta=0.0)
+        B.normtest_clip_grads(g, norms, out=lists[3])
+        B.normtest_clip_grads(g, norms)
+        if path:
+            assert fast.back == [B.NT_OK] * 8
+        results.append([t.clone() for t in (*x, *w, *m, *v, *c, norms, after)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    monkeypatch.setattr(B, "_fast", fast)
+    # what the native path does not take goes through Python, which takes or refuses it
+    odd = B.make_tensor_list([t.as_subclass(Other) for t in x], like=g)
+    before = [t.clone() for t in c]
+    fast.back = []
+    B.normtest_clip_grads(lists[3], norms, out=odd)
+    B.normtest_grad_norm(g, norms, max_norm=1)
+    B.normtest_grad_norm(g, norms, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert fast.back == [None, None] and all(torch.equal(a, b) for a, b in zip(before, c))
+    other = B.make_tensor_list([t.clone() for t in x], groups=[0, 1, 0])
+    for call in [lambda: B.normtest_clip_grads(g, norms, out=other), lambda: B.normtest_accumulate(g, other), lambda: B.normtest_accumulate(g, None),
+                 lambda: B.normtest_accumulate(g, x), lambda: B.normtest_clip_grads(g, norms, out=x), lambda: B.normtest_grad_norm(g, norms[:8]),
+                 lambda: B.normtest_clip_grads(g, None), lambda: B.normtest_clip_grads(g, norms.cpu()), lambda: B.normtest_grad_norm(g, norms, kind=9),
+                 lambda: B.normtest_grad_norm(g, norms, kind=-1), lambda: B.normtest_adamw_tensors(g, *lists[:2], lists[3], hyper()),
+                 lambda: B.normtest_adamw_tensors(g, *lists[:3], None), lambda: B.normtest_adamw_tensors(g, *lists[:3], hyper(), copy=other)]:
+        raised = []
+        for path in (fast, None):
+            monkeypatch.setattr(B, "_fast", path)
+            with pytest.raises(Exception) as e:
+                call()
+            raised.append((type(e.value), str(e.value)))
+        assert raised[0] == raised[1]
+    monkeypatch.setattr(B, "_fast", fast)
+    x[0].data = x[0].clone()
+    with pytest.raises(RuntimeError, match="refresh"):
+        B.normtest_grad_norm(g, norms)
+
+
 def test_streams_and_graphs():
     shapes = [(50_000,), (70, 900), (3,)]
     x, _ = carve(shapes, [BF16, F32, F16], 40, extra=2)
