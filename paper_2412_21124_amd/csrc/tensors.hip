@@ -21,39 +21,27 @@
 #include "normtest.h"
 
 #define NT_ITEM 4096            // elements of an item of the kernels that write
-#ifndef NT_THREADS
 #define NT_THREADS 256          // threads of a block of the update
+#define NT_ADAMW_THREADS 512    // threads of a block of AdamW
+#ifndef NT_STEP_LIST
+#define NT_STEP_LIST (5ll << 23)   // elements from which its blocks are kept in step: one block of a CU, many launches
 #endif
-#ifndef NT_ADAMW_THREADS
-#define NT_ADAMW_THREADS 512
-#endif
+#define NT_STEP_THREADS 1024    // then: an item in one sweep,
+#define NT_STEP_LDS 82000       // more than half of a CU's LDS, so that one block fits,
+#define NT_STEP_ITEMS 16384     // items of a launch
 #define NT_NORM_THREADS 256     // threads of a block of the norm's kernel
 #define NT_NORM_FLIGHT 4        // 16-byte loads that a thread of it has in flight
 #define NT_LONG_ITEM 8192       // elements of its items in a long list
+#ifndef NT_LONG_BLOCKS
 #define NT_LONG_BLOCKS 1024     // and its blocks, which walk such a list
+#endif
 #define NT_LONG_LIST (1ll << 23)   // elements from which a list is long
 #define NT_MOST_BLOCKS (1u << 20)  // blocks of one launch
-#ifndef NT_ADAMW_LAUNCH
-#define NT_ADAMW_LAUNCH NT_MOST_BLOCKS
-#endif
-#ifndef UPD_NT_X
-#define UPD_NT_X false
-#endif
-#ifndef UPD_NT_Y
-#define UPD_NT_Y false
-#endif
-#ifndef ADAMW_NT_G
-#define ADAMW_NT_G false
-#endif
-#ifndef ADAMW_NT_S
-#define ADAMW_NT_S false
-#endif
-#ifndef NT_ADAMW_LDS
-#define NT_ADAMW_LDS 0
-#endif
 // Elements from which loads (and stores) go past the 256 MB cache that the chip's memory has, because what they touch would not stay in it
 // until it is needed again.
-#define NT_STREAM_NORM (1ll << 27)
+#define NT_STREAM_READ (1ll << 27)     // what is only read: gradients, which the norm's kernel leaves there for the next call
+#define NT_STREAM_UPDATE (3ll << 23)   // what an update writes
+#define NT_STREAM_ADAMW (1ll << 23)    // weights and moments
 #define NT_PLAN_MAGIC 0x4e54504cu
 #define NT_COUNTER_WORDS 16     // a counter has 64 bytes of its own, so that counting blocks of different slabs do not meet
 
@@ -112,7 +100,12 @@ struct Cut {
 struct Layout {
   size_t shapes, items[2], groups[2], counters[2], upload, partials[2], sums[2], bytes;
 };
-constexpr uint32_t BLOCKS[2] = {1u << 31, NT_LONG_BLOCKS};   // items of the first cut have a block each
+// Blocks that take a cut's items, which for the first cut is a block for each.  The norm's kernel walks a long list with few, unless its
+// groups are so short that a block would meet another one, and end a part, with almost every item.
+uint32_t blocks_of(const nt_plan& p, int k) {
+  if (k == 0) return 1u << 31;
+  return p.items[1] >= (int64_t)p.groups * 4 * NT_LONG_BLOCKS ? NT_LONG_BLOCKS : 1u << 23;
+}
 constexpr int64_t SIZES[2] = {NT_ITEM, NT_LONG_ITEM};
 // A slab is all slots, or about as many as there are slabs, so that neither counter is counted up often: a counter takes some 10 ns
 // per block, a second level some 3 us.
@@ -213,31 +206,98 @@ __device__ inline void store_part(int dtype, char NT_GLOBAL* p, const u32x4& r, 
     }
 }
 
-// Where group q of four elements of an item lies: row and first column, and how many of the four there are (at most 0: none).
-struct Spot {
-  int64_t row, col;
-  int n;
+// The elements of an item that is not a whole one of a tensor of one row, four at a time: quad c of the item's row r.  A thread takes
+// every THREADS-th quad; only its first place takes a division by the row's quads, which differ from tensor to tensor.
+template <int THREADS>
+struct Walk {
+  int64_t row0, col0;                 // of the item
+  uint32_t rows, width, quads;        // of the item
+  uint32_t r, c, dr, dc;
+  bool wrapped;
+  __device__ inline Walk() {}
+  __device__ inline Walk(const Item& it, const Shape* shapes, int level, uint32_t size) {
+    if (it.count & NT_ROWS) {
+      const Shape NT_CONST* s = constant(shapes) + it.tensor;
+      const uint32_t per_row = s->per_row[level];
+      row0 = per_row ? it.idx / per_row : (int64_t)it.idx * s->rows_per_item[level];
+      col0 = per_row ? (int64_t)(it.idx % per_row) * size : 0;
+      rows = it.count & ~NT_ROWS;
+      const int64_t left = s->cols - col0;
+      width = left < size ? (uint32_t)left : size;
+    } else {
+      row0 = 0;
+      col0 = (int64_t)it.idx * size;
+      rows = 1;
+      width = it.count;
+    }
+    quads = (width + 3) / 4;
+    r = threadIdx.x / quads;
+    c = threadIdx.x % quads;
+    dr = THREADS / quads;
+    dc = THREADS % quads;
+  }
+  // how many elements there are at this place: 0 past the item's end
+  __device__ inline int here() const {
+    const uint32_t left = width - 4 * c;
+    return r < rows ? (int)(left < 4 ? left : 4) : 0;
+  }
+  __device__ inline void step() {
+    r += dr;
+    c += dc;
+    wrapped = c >= quads;
+    if (wrapped) {
+      c -= quads;
+      ++r;
+    }
+  }
 };
-__device__ inline Spot spot(const Item& it, const Shape* shapes, int level, int64_t size, uint32_t q) {
-  if (!(it.count & NT_ROWS)) {
-    const int64_t left = (int64_t)it.count - 4 * (int64_t)q;
-    return {0, it.idx * size + 4 * (int64_t)q, (int)(left < 4 ? left : 4)};
+// The walk's place in one tensor, in bytes from the item's first element; it steps behind the walk.
+template <int DTYPE>
+struct Place {
+  char NT_GLOBAL* base;      // of the item, the same for the whole block
+  uint64_t off, by, wrap;    // by: of a step; wrap: more where it goes on to another row
+  template <class W>
+  __device__ inline Place(const nt_tensor NT_CONST* t, const W& at) {
+    const uint64_t ld = t->ld;
+    constexpr int shift = DTYPE == NT_F32 ? 2 : 1;
+    base = (char NT_GLOBAL*)t->data + ((at.row0 * (int64_t)ld + at.col0) << shift);
+    off = (at.r * ld + 4 * at.c) << shift;
+    by = (at.dr * ld + 4 * at.dc) << shift;
+    wrap = (ld - 4 * (uint64_t)at.quads) << shift;
   }
-  const Shape NT_CONST* s = constant(shapes) + it.tensor;
-  const int64_t cols = s->cols;
-  const uint32_t per_row = s->per_row[level], count = it.count & ~NT_ROWS;
-  if (per_row) {
-    const int64_t row = it.idx / per_row, col = (it.idx % per_row) * size + 4 * (int64_t)q;
-    const int64_t end = (it.idx % per_row + 1) * size, left = (end < cols ? end : cols) - col;
-    return {row, col, (int)(left < 4 ? (left < 0 ? 0 : left) : 4)};
+  template <class W>
+  __device__ inline void step(const W& at) {
+    off += at.wrapped ? by + wrap : by;
   }
-  const uint32_t quads = (uint32_t)((cols + 3) / 4);
-  const uint32_t r = q / quads, c = 4 * (q % quads);
-  const int64_t left = r < count ? cols - c : 0;
-  return {(int64_t)it.idx * s->rows_per_item[level] + r, c, (int)(left < 4 ? left : 4)};
-}
-__device__ inline char NT_GLOBAL* address(const nt_tensor NT_CONST* t, int dtype, const Spot& s) {
-  return (char NT_GLOBAL*)t->data + ((s.row * t->ld + s.col) << size_shift(dtype));
+  // The n elements here.  A row's last one to three are loaded with the same instruction as four, from four before the row's end on, and
+  // settle() moves them down; what else it loads is its neighbour's, which may have been written by then, and is moved out.  Element by
+  // element they were a chain of loads in every wave that meets a row's end.  (Two functions, so that several loads are under way.)
+  template <class W>
+  __device__ inline u32x4 load(const W& at, int n) const {
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (at.width < 4)
+      x = load_part(DTYPE, base + off, n);
+    else if (n > 0)
+      x = load4(DTYPE, base + (off - ((uint64_t)(uint32_t)(4 - n) << size_shift(DTYPE))));
+    return x;
+  }
+  template <class W>
+  __device__ static inline u32x4 settle(const W& at, const u32x4& x, int n) {
+    if (n == 4 || at.width < 4) return x;
+    const int back = 4 - n;   // 4: no element, and zeros already
+    if (DTYPE == NT_F32) {
+      const u32x4 y = back & 1 ? u32x4{x[1], x[2], x[3], 0u} : x;
+      return back & 2 ? u32x4{y[2], y[3], 0u, 0u} : y;
+    }
+    const uint64_t y = ((uint64_t)x[1] << 32 | x[0]) >> (16 * back & 63);
+    return u32x4{(uint32_t)y, (uint32_t)(y >> 32), 0u, 0u};
+  }
+};
+__device__ inline void store_n(int dtype, char NT_GLOBAL* p, const u32x4& x, int n) {
+  if (n == 4)
+    store4(dtype, p, x);
+  else
+    store_part(dtype, p, x, n);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -452,29 +512,28 @@ __device__ inline void norm_flat(const char NT_GLOBAL* p, uint32_t n, typename K
   total = K::join(acc[0], acc[1]);
 }
 // An item of a tensor with rows, four elements at a time.
-template <class K>
+template <class K, int DTYPE>
 __device__ inline void norm_rows(const nt_tensor NT_CONST* t, const Item& it, const Shape* shapes, int level, uint32_t size,
                                  typename K::T& acc) {
-  constexpr int FLIGHT = 4;
-  const int dtype = t->dtype;
-  for (uint32_t q0 = threadIdx.x; q0 < size / 4; q0 += FLIGHT * NT_NORM_THREADS) {
-    u32x4 r[FLIGHT];
+  constexpr int FLIGHT = 8;
+  Walk<NT_NORM_THREADS> at(it, shapes, level, size);
+  Place<DTYPE> place(t, at);
+  for (uint32_t done = 0; done < at.rows * at.quads; done += FLIGHT * NT_NORM_THREADS) {
+    u32x4 x[FLIGHT];
+    int n[FLIGHT];
 #pragma unroll
     for (int k = 0; k < FLIGHT; ++k) {
-      const uint32_t q = q0 + k * NT_NORM_THREADS;
-      const Spot s = spot(it, shapes, level, size, q);
-      const int n = q < size / 4 ? s.n : 0;
-      const char NT_GLOBAL* p = address(t, dtype, s);
-      if (n == 4)
-        r[k] = load4(dtype, p);
-      else
-        r[k] = load_part(dtype, p, n);
+      n[k] = at.here();
+      x[k] = place.load(at, n[k]);
+      at.step();
+      place.step(at);
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < FLIGHT; ++k) {
-      const f32x4 x = values(dtype, r[k]);   // zeros, which add nothing, where there are no elements
+      const f32x4 v = values(DTYPE, place.settle(at, x[k], n[k]));   // zeros, which add nothing, where there are no elements
 #pragma unroll
-      for (int e = 0; e < 4; ++e) K::add(acc, x[e]);
+      for (int e = 0; e < 4; ++e) K::add(acc, v[e]);
     }
   }
 }
@@ -505,7 +564,7 @@ __global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_t
       dtype = nt->dtype;
     }
     if (it.count & NT_ROWS)
-      norm_rows<K>(t, it, a.shapes, level, size, acc);
+      by_type(type, [&](auto d) { norm_rows<K, decltype(d)::value>(t, it, a.shapes, level, size, acc); });
     else if (it.count)
       by_type(type, [&](auto d) { norm_flat<K, decltype(d)::value, STREAM>(from, it.count, acc); });
     if (!more || nx.group != it.group) {
@@ -528,8 +587,11 @@ struct UpdateArgs {
   float beta;
   int in_place;           // dst is src, and nothing is to be done where the factor is 1
 };
+// What of a call goes past the caches: nothing, what it writes (and reads there), or what it only reads too.
+enum { KEEP = 0, STREAM_WRITTEN = 1, STREAM_ALL = 2 };
+
 // A whole item of a tensor of one row: all loads, then all stores.
-template <bool READ, class K, int XT, int YT, class ACC>
+template <bool READ, class K, int STREAM, int XT, int YT, class ACC>
 __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, float scale, float beta, ACC& acc) {
   constexpr int PER = XT != NT_F32 && YT != NT_F32 ? 8 : 4, SWEEPS = NT_ITEM / (PER * NT_THREADS);
   static_assert(SWEEPS * PER * NT_THREADS == NT_ITEM, "an item is whole sweeps");
@@ -540,8 +602,8 @@ __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, f
   const uint32_t lane = PER * threadIdx.x;
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    xr[k] = X::template load<UPD_NT_X>(x + X::SIZE * (lane + k * PER * NT_THREADS));
-    if constexpr (READ) yr[k] = Y::template load<UPD_NT_Y>(y + Y::SIZE * (lane + k * PER * NT_THREADS));
+    xr[k] = X::template load<STREAM == STREAM_ALL>(x + X::SIZE * (lane + k * PER * NT_THREADS));
+    if constexpr (READ) yr[k] = Y::template load<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * NT_THREADS));
   }
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -552,51 +614,48 @@ __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, f
       const float v = X::value(xr[k], e);
       Y::put(z, e, READ ? __builtin_fmaf(scale, v, beta * Y::value(yr[k], e)) : scale * v);
     }
-    Y::template store<UPD_NT_Y>(y + Y::SIZE * (lane + k * PER * NT_THREADS), z);
+    Y::template store<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * NT_THREADS), z);
     if constexpr (!__is_same(K, void)) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) K::add(acc, Y::value(z, e));
     }
   }
 }
-// Any item, four elements at a time.
-template <bool READ, class K, class ACC>
-__device__ inline void update_any(const nt_tensor NT_CONST* x, const nt_tensor NT_CONST* y, const Item& it, const Shape* shapes, float scale,
-                                  float beta, ACC& acc) {
+// Any other item.
+template <bool READ, class K, int XT, int YT, class ACC>
+__device__ inline void update_walk(const nt_tensor NT_CONST* x, const nt_tensor NT_CONST* y, const Item& it, const Shape* shapes, float scale,
+                                   float beta, ACC& acc) {
   constexpr int SWEEPS = NT_ITEM / (4 * NT_THREADS);
-  const int xt = x->dtype, yt = y->dtype;
-  Spot s[SWEEPS];
+  Walk<NT_THREADS> at(it, shapes, 0, NT_ITEM);
+  Place<XT> from(x, at);
+  Place<YT> to(y, at);
   u32x4 xr[SWEEPS], yr[SWEEPS];
+  uint64_t off[SWEEPS];
+  int n[SWEEPS];
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    s[k] = spot(it, shapes, 0, NT_ITEM, threadIdx.x + k * NT_THREADS);
-    const char NT_GLOBAL* from = address(x, xt, s[k]);
-    const char NT_GLOBAL* to = address(y, yt, s[k]);
-    if (s[k].n == 4) {
-      xr[k] = load4(xt, from);
-      if constexpr (READ) yr[k] = load4(yt, to);
-    } else {
-      xr[k] = load_part(xt, from, s[k].n);
-      if constexpr (READ) yr[k] = load_part(yt, to, s[k].n);
-    }
+    n[k] = at.here();
+    off[k] = to.off;
+    xr[k] = from.load(at, n[k]);
+    if constexpr (READ) yr[k] = to.load(at, n[k]);
+    at.step();
+    from.step(at);
+    to.step(at);
   }
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    const f32x4 xv = values(xt, xr[k]);
+    const f32x4 xv = values(XT, from.settle(at, xr[k], n[k]));
     f32x4 yv = {0.f, 0.f, 0.f, 0.f}, z;
-    if constexpr (READ) yv = values(yt, yr[k]);
+    if constexpr (READ) yv = values(YT, to.settle(at, yr[k], n[k]));
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = READ ? __builtin_fmaf(scale, xv[e], beta * yv[e]) : scale * xv[e];
-    const u32x4 zr = rounded(yt, z);
-    char NT_GLOBAL* to = address(y, yt, s[k]);
-    if (s[k].n == 4)
-      store4(yt, to, zr);
-    else
-      store_part(yt, to, zr, s[k].n);
+    const u32x4 zr = rounded(YT, z);
+    store_n(YT, to.base + off[k], zr, n[k]);
     if constexpr (!__is_same(K, void)) {
-      const f32x4 v = values(yt, zr);
+      const f32x4 v = values(YT, zr);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) K::add(acc, e < s[k].n ? v[e] : 0.f);
+      for (int e = 0; e < 4; ++e) K::add(acc, e < n[k] ? v[e] : 0.f);
     }
   }
 }
@@ -609,7 +668,7 @@ struct Partial<void> {
   typedef int T;
 };
 // dst <- beta dst + scale factor src
-template <bool READ, class K>
+template <bool READ, class K, int STREAM>
 __global__ __launch_bounds__(NT_THREADS) void k_update(ListArgs a, UpdateArgs u, NormOut o) {
   const uint32_t item = a.item0 + blockIdx.x;
   const Item it = item_at(a.items, item);
@@ -623,16 +682,18 @@ __global__ __launch_bounds__(NT_THREADS) void k_update(ListArgs a, UpdateArgs u,
       if (u.in_place && factor == 1.f) return;
       scale = (float)(u.scale * (double)factor);
     }
+    const int xt = x->dtype, yt = y->dtype;
     if (it.count == NT_ITEM) {
-      const int xt = x->dtype, yt = y->dtype;
       const uint64_t at = (uint64_t)it.idx * NT_ITEM;
       const char NT_GLOBAL* from = (const char NT_GLOBAL*)x->data + (at << size_shift(xt));
       char NT_GLOBAL* to = (char NT_GLOBAL*)y->data + (at << size_shift(yt));
       by_type(xt, [&](auto dx) {
-        by_type(yt, [&](auto dy) { update_flat<READ, K, decltype(dx)::value, decltype(dy)::value>(from, to, scale, u.beta, acc); });
+        by_type(yt, [&](auto dy) { update_flat<READ, K, STREAM, decltype(dx)::value, decltype(dy)::value>(from, to, scale, u.beta, acc); });
       });
     } else {
-      update_any<READ, K>(x, y, it, a.shapes, scale, u.beta, acc);
+      by_type(xt, [&](auto dx) {
+        by_type(yt, [&](auto dy) { update_walk<READ, K, decltype(dx)::value, decltype(dy)::value>(x, y, it, a.shapes, scale, u.beta, acc); });
+      });
     }
   }
   if constexpr (!__is_same(K, void)) end_part<K, NT_THREADS>(o, item, it.group, acc);
@@ -662,10 +723,11 @@ __device__ inline void adamw_element(const AdamwArgs& p, float g, float& w, floa
   w = __builtin_fmaf(p.decay, w, -upd);
 }
 // A whole item of a tensor of one row.
-template <int GT>
+template <int GT, int STREAM, int THREADS>
 __device__ inline void adamw_flat(const AdamwArgs& u, const char NT_GLOBAL* gp, char NT_GLOBAL* wp, char NT_GLOBAL* mp, char NT_GLOBAL* vp,
                                   char NT_GLOBAL* cp, int copy_type, float scale) {
-  constexpr int SWEEPS = NT_ITEM / (4 * NT_ADAMW_THREADS);
+  constexpr int SWEEPS = NT_ITEM / (4 * THREADS);
+  constexpr bool S = STREAM != KEEP;
   typedef Vec<GT, 4> G;
   typedef Vec<NT_F32, 4> F;
   typename G::raw_t g[SWEEPS];
@@ -673,16 +735,16 @@ __device__ inline void adamw_flat(const AdamwArgs& u, const char NT_GLOBAL* gp, 
   const uint32_t lane = 4 * threadIdx.x;
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    const uint32_t at = lane + k * 4 * NT_ADAMW_THREADS;
-    g[k] = G::template load<ADAMW_NT_G>(gp + G::SIZE * at);
-    w[k] = F::template load<ADAMW_NT_S>(wp + 4 * at);
-    m[k] = F::template load<ADAMW_NT_S>(mp + 4 * at);
-    v[k] = F::template load<ADAMW_NT_S>(vp + 4 * at);
+    const uint32_t at = lane + k * 4 * THREADS;
+    g[k] = G::template load<STREAM == STREAM_ALL>(gp + G::SIZE * at);
+    w[k] = F::template load<S>(wp + 4 * at);
+    m[k] = F::template load<S>(mp + 4 * at);
+    v[k] = F::template load<S>(vp + 4 * at);
   }
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    const uint32_t at = lane + k * 4 * NT_ADAMW_THREADS;
+    const uint32_t at = lane + k * 4 * THREADS;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float we = F::value(w[k], e), me = F::value(m[k], e), ve = F::value(v[k], e);
@@ -691,53 +753,70 @@ __device__ inline void adamw_flat(const AdamwArgs& u, const char NT_GLOBAL* gp, 
       F::put(m[k], e, me);
       F::put(v[k], e, ve);
     }
-    F::template store<ADAMW_NT_S>(wp + 4 * at, w[k]);
-    F::template store<ADAMW_NT_S>(mp + 4 * at, m[k]);
-    F::template store<ADAMW_NT_S>(vp + 4 * at, v[k]);
-    if (cp) store4(copy_type, cp + (at << size_shift(copy_type)), rounded(copy_type, __builtin_bit_cast(f32x4, w[k])));
+    F::template store<S>(wp + 4 * at, w[k]);
+    F::template store<S>(mp + 4 * at, m[k]);
+    F::template store<S>(vp + 4 * at, v[k]);
+    // the copy is what the next forward pass reads first
+    if (cp) store4(copy_type, cp + ((uint64_t)at << size_shift(copy_type)), rounded(copy_type, __builtin_bit_cast(f32x4, w[k])));
   }
 }
-// Four elements, or the n of them that there are.
-__device__ inline void adamw_any(const AdamwArgs& u, const nt_tensor NT_CONST* gt, const nt_tensor NT_CONST* wt, const nt_tensor NT_CONST* mt,
-                                 const nt_tensor NT_CONST* vt, const nt_tensor NT_CONST* ct, const Spot& s, float scale) {
-  if (s.n <= 0) return;
-  const int dtype = gt->dtype;
-  const char NT_GLOBAL* gp = address(gt, dtype, s);
-  char NT_GLOBAL *wp = address(wt, NT_F32, s), *mp = address(mt, NT_F32, s), *vp = address(vt, NT_F32, s);
-  u32x4 gr, wr, mr, vr;
-  if (s.n == 4) {
-    gr = load4(dtype, gp);
-    wr = load4(NT_F32, wp);
-    mr = load4(NT_F32, mp);
-    vr = load4(NT_F32, vp);
-  } else {
-    gr = load_part(dtype, gp, s.n);
-    wr = load_part(NT_F32, wp, s.n);
-    mr = load_part(NT_F32, mp, s.n);
-    vr = load_part(NT_F32, vp, s.n);
-  }
-  const f32x4 g = values(dtype, gr);
-  f32x4 w = __builtin_bit_cast(f32x4, wr), m = __builtin_bit_cast(f32x4, mr), v = __builtin_bit_cast(f32x4, vr);
+// Any other item.
+template <int GT, int THREADS>
+__device__ inline void adamw_walk(const AdamwArgs& u, const nt_tensor NT_CONST* gt, const nt_tensor NT_CONST* wt, const nt_tensor NT_CONST* mt,
+                                  const nt_tensor NT_CONST* vt, const nt_tensor NT_CONST* ct, const Item& it, const Shape* shapes, float scale) {
+  constexpr int SWEEPS = NT_ITEM / (4 * THREADS);
+  Walk<THREADS> at(it, shapes, 0, NT_ITEM);
+  Place<GT> gp(gt, at);
+  Place<NT_F32> wp(wt, at), mp(mt, at), vp(vt, at);
+  u32x4 gr[SWEEPS], wr[SWEEPS], mr[SWEEPS], vr[SWEEPS];
+  uint64_t wo[SWEEPS], mo[SWEEPS], vo[SWEEPS];
+  uint32_t r[SWEEPS], c[SWEEPS];
+  int n[SWEEPS];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float we = w[e], me = m[e], ve = v[e];
-    adamw_element(u, scale * g[e], we, me, ve);
-    w[e] = we;
-    m[e] = me;
-    v[e] = ve;
+  for (int k = 0; k < SWEEPS; ++k) {
+    n[k] = at.here();
+    r[k] = at.r;
+    c[k] = at.c;
+    wo[k] = wp.off;
+    mo[k] = mp.off;
+    vo[k] = vp.off;
+    gr[k] = gp.load(at, n[k]);
+    wr[k] = wp.load(at, n[k]);
+    mr[k] = mp.load(at, n[k]);
+    vr[k] = vp.load(at, n[k]);
+    at.step();
+    gp.step(at);
+    wp.step(at);
+    mp.step(at);
+    vp.step(at);
   }
-  auto put = [&](int type, char NT_GLOBAL* p, const u32x4& r) {
-    if (s.n == 4)
-      store4(type, p, r);
-    else
-      store_part(type, p, r, s.n);
-  };
-  put(NT_F32, wp, __builtin_bit_cast(u32x4, w));
-  put(NT_F32, mp, __builtin_bit_cast(u32x4, m));
-  put(NT_F32, vp, __builtin_bit_cast(u32x4, v));
-  if (ct) put(ct->dtype, address(ct, ct->dtype, s), rounded(ct->dtype, w));
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int k = 0; k < SWEEPS; ++k) {
+    if (n[k] == 0) continue;
+    const f32x4 g = values(GT, gp.settle(at, gr[k], n[k]));
+    f32x4 w = values(NT_F32, wp.settle(at, wr[k], n[k])), m = values(NT_F32, mp.settle(at, mr[k], n[k])),
+          v = values(NT_F32, vp.settle(at, vr[k], n[k]));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float we = w[e], me = m[e], ve = v[e];
+      adamw_element(u, scale * g[e], we, me, ve);
+      w[e] = we;
+      m[e] = me;
+      v[e] = ve;
+    }
+    store_n(NT_F32, wp.base + wo[k], __builtin_bit_cast(u32x4, w), n[k]);
+    store_n(NT_F32, mp.base + mo[k], __builtin_bit_cast(u32x4, m), n[k]);
+    store_n(NT_F32, vp.base + vo[k], __builtin_bit_cast(u32x4, v), n[k]);
+    if (ct) {
+      const int type = ct->dtype;
+      const uint64_t at_copy = (at.row0 + r[k]) * ct->ld + at.col0 + 4 * c[k];
+      store_n(type, (char NT_GLOBAL*)ct->data + (at_copy << size_shift(type)), rounded(type, w), n[k]);
+    }
+  }
 }
-__global__ __launch_bounds__(NT_ADAMW_THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
+template <int STREAM, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
   const Item it = item_at(a.items, a.item0 + blockIdx.x);
   if (!it.count) return;
   const nt_tensor NT_CONST* gt = constant(u.grads) + it.tensor;
@@ -751,19 +830,18 @@ __global__ __launch_bounds__(NT_ADAMW_THREADS) void k_adamw(ListArgs a, AdamwArg
     if ((u.flags & NT_SKIP_NONFINITE) && (n->status & NT_STATUS_NONFINITE)) return;
     scale = (float)u.grad_scale * n->factor;
   }
+  const int dtype = gt->dtype;
   if (it.count == NT_ITEM) {
     const uint64_t at = (uint64_t)it.idx * NT_ITEM;
-    const int dtype = gt->dtype, copy_type = ct ? ct->dtype : 0;
+    const int copy_type = ct ? ct->dtype : 0;
     const char NT_GLOBAL* gp = (const char NT_GLOBAL*)gt->data + (at << size_shift(dtype));
     char NT_GLOBAL* cp = ct ? (char NT_GLOBAL*)ct->data + (at << size_shift(copy_type)) : nullptr;
     by_type(dtype, [&](auto d) {
-      adamw_flat<decltype(d)::value>(u, gp, (char NT_GLOBAL*)wt->data + 4 * at, (char NT_GLOBAL*)mt->data + 4 * at,
-                                     (char NT_GLOBAL*)vt->data + 4 * at, cp, copy_type, scale);
+      adamw_flat<decltype(d)::value, STREAM, THREADS>(u, gp, (char NT_GLOBAL*)wt->data + 4 * at, (char NT_GLOBAL*)mt->data + 4 * at,
+                                             (char NT_GLOBAL*)vt->data + 4 * at, cp, copy_type, scale);
     });
   } else {
-#pragma unroll 1
-    for (uint32_t q = threadIdx.x; q < NT_ITEM / 4; q += NT_ADAMW_THREADS)
-      adamw_any(u, gt, wt, mt, vt, ct, spot(it, a.shapes, 0, NT_ITEM, q), scale);
+    by_type(dtype, [&](auto d) { adamw_walk<decltype(d)::value, THREADS>(u, gt, wt, mt, vt, ct, it, a.shapes, scale); });
   }
 }
 
@@ -789,7 +867,7 @@ Pieces pieces_of(int64_t rows, int64_t cols, int64_t size) {
 Cut cut_of(const nt_plan& p, const Layout& l, int k) {
   char* const b = (char*)p.image;
   return {(const Item*)(b + l.items[k]), (const Group*)(b + l.groups[k]), (uint32_t*)(b + l.counters[k]), (double*)(b + l.partials[k]),
-          (double*)(b + l.sums[k]), p.items[k], p.slabs[k], BLOCKS[k], slab_shift(p.slots[k])};
+          (double*)(b + l.sums[k]), p.items[k], p.slabs[k], blocks_of(p, k), slab_shift(p.slots[k])};
 }
 
 int check_plan(const nt_plan* p) {
@@ -817,19 +895,24 @@ int in_launches(uint32_t items, uint32_t most, LAUNCH launch) {
   return NT_OK;
 }
 
-template <bool READ>
+template <bool READ, int STREAM>
 int enqueue_update(const nt_plan& p, const Layout& l, const UpdateArgs& u, int kind, const NormOut& o, hipStream_t st) {
-  const Cut cut = cut_of(p, l, 0);
-  ListArgs a = {(const Shape*)((char*)p.image + l.shapes), cut.items, 0};
+  ListArgs a = {(const Shape*)((char*)p.image + l.shapes), cut_of(p, l, 0).items, 0};
   return in_launches(p.items[0], NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
     if (!o.norms)
-      hipLaunchKernelGGL((k_update<READ, void>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, void, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
     else if (kind == NT_NORM_L2)
-      hipLaunchKernelGGL((k_update<READ, Square>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, Square, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
     else
-      hipLaunchKernelGGL((k_update<READ, Largest>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, Largest, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
   });
+}
+template <bool READ>
+int enqueue_update(const nt_plan& p, const Layout& l, const UpdateArgs& u, int kind, const NormOut& o, hipStream_t st) {
+  if (p.elements < NT_STREAM_UPDATE) return enqueue_update<READ, KEEP>(p, l, u, kind, o, st);
+  return p.elements < NT_STREAM_READ ? enqueue_update<READ, STREAM_WRITTEN>(p, l, u, kind, o, st)
+                                     : enqueue_update<READ, STREAM_ALL>(p, l, u, kind, o, st);
 }
 
 }  // namespace
@@ -878,18 +961,17 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
     for (int64_t j = group_begin(g); j < first[g]; ++j) n += pieces_of(tensors[order[j]].rows, tensors[order[j]].cols, SIZES[k]).n;
     return n ? n : 1;
   };
-  auto slots_of = [](int64_t items, int k) { return items < BLOCKS[k] ? items : (int64_t)BLOCKS[k]; };
+  auto slots_of = [&](int64_t items, int k) { return items < blocks_of(p, k) ? items : (int64_t)blocks_of(p, k); };
   for (int k = 0; k < cuts; ++k) {
     int64_t items = 0, slots = 0, slabs = 0;
     for (int32_t g = 0; g < G; ++g) {
-      const int64_t here = items_of(g, k);
-      items += here;
-      slots += slots_of(here, k);
+      items += items_of(g, k);
       if (items > (1ll << 31) - 1) return NT_ERR_TOO_LARGE;
     }
+    p.items[k] = (uint32_t)items;
+    for (int32_t g = 0; g < G; ++g) slots += slots_of(items_of(g, k), k);
     const int shift = slab_shift((uint32_t)slots);
     for (int32_t g = 0; g < G; ++g) slabs += ceil_div(slots_of(items_of(g, k), k), 1ll << shift);
-    p.items[k] = (uint32_t)items;
     p.slots[k] = (uint32_t)slots;
     p.slabs[k] = (uint32_t)slabs;
   }
@@ -967,7 +1049,7 @@ int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind
   const NormOut o = {cut_of(*plan, l, k), max_norm, grad_scale, norms};
   const ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), o.cut.items, 0};
   const uint32_t blocks = o.cut.nitems < o.cut.blocks ? o.cut.nitems : o.cut.blocks;
-  const bool stream = plan->elements >= NT_STREAM_NORM;
+  const bool stream = plan->elements >= NT_STREAM_READ;
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT_NORM_THREADS), 0, (hipStream_t)hip_stream, a, grads, k, o);
     return hip_code(hipGetLastError());
@@ -1028,9 +1110,18 @@ int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt
   const Cut cut = cut_of(*plan, l, 0);
   ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), cut.items, 0};
   hipStream_t st = (hipStream_t)hip_stream;
-  return in_launches(plan->items[0], NT_ADAMW_LAUNCH, [&](uint32_t at, uint32_t n) {
+  const bool step = plan->elements >= NT_STEP_LIST;
+  return in_launches(plan->items[0], step ? NT_STEP_ITEMS : NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
-    hipLaunchKernelGGL(k_adamw, dim3(n), dim3(NT_ADAMW_THREADS), NT_ADAMW_LDS, st, a, u);
+    auto launch = [&](auto kernel, int threads, int lds) { hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), lds, st, a, u); };
+    if (plan->elements < NT_STREAM_ADAMW)
+      launch(k_adamw<KEEP, NT_ADAMW_THREADS>, NT_ADAMW_THREADS, 0);
+    else if (!step)
+      launch(k_adamw<STREAM_WRITTEN, NT_ADAMW_THREADS>, NT_ADAMW_THREADS, 0);
+    else if (plan->elements < NT_STREAM_READ)
+      launch(k_adamw<STREAM_WRITTEN, NT_STEP_THREADS>, NT_STEP_THREADS, NT_STEP_LDS);
+    else
+      launch(k_adamw<STREAM_ALL, NT_STEP_THREADS>, NT_STEP_THREADS, NT_STEP_LDS);
   });
 }
 

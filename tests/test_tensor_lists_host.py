@@ -115,14 +115,14 @@ def test_slots_and_slabs_are_a_groups_own(seed):
     rng = random.Random(seed)
     shapes = [rng.choice([(1, 0), (1, rng.randrange(1, 40000)), (rng.randrange(2, 300), rng.randrange(1, 900))]) for _ in range(rng.choice([1, 40, 300]))]
     if seed % 2:
-        shapes += [(1, rng.randrange(1 << 23, 1 << 25)), (1 << 12, rng.randrange(100, 9000))]
+        shapes += [(1, rng.randrange(1 << 23, 1 << 26)), (1 << 12, rng.randrange(100, 9000))]
     G = rng.choice([1, 3, 50])
     groups = [rng.randrange(G) for _ in shapes]
     plan, image = plan_of(shapes, groups, G)
     _, cuts = cuts_of(plan, image)
     assert len(cuts) == (2 if plan.elements >= 1 << 23 else 1)
     for k, (items, grps, _) in enumerate(cuts):
-        blocks = [1 << 31, 1024][k]
+        blocks = [1 << 31, 1024 if plan.items[1] >= 4096 * G else 1 << 23][k]
         shift = slab_shift(plan.slots[k])
         assert (np.diff(items["group"].astype(np.int64)) >= 0).all() and set(items["group"]) == set(range(G))
         parts = {}   # group -> slots in the order of their blocks
