@@ -344,7 +344,7 @@ typedef struct {
   int64_t elements;        /* of all tensors */
   int32_t tensors, groups; /* N, G */
   uint32_t items[2], slots[2], slabs[2];
-  uint32_t magic, reserved;
+  uint32_t magic, flags;
 } nt_plan;
 
 /* Which norm */

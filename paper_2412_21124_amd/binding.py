@@ -91,7 +91,7 @@ class nt_plan(ctypes.Structure):
     _fields_ = [("image", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("upload_bytes", ctypes.c_size_t), ("elements", ctypes.c_int64),
                 ("tensors", ctypes.c_int32), ("groups", ctypes.c_int32), ("items", ctypes.c_uint32 * 2), ("slots", ctypes.c_uint32 * 2),
                 ("slabs", ctypes.c_uint32 * 2),
-                ("magic", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+                ("magic", ctypes.c_uint32), ("flags", ctypes.c_uint32)]
 
 
 class nt_norm(ctypes.Structure):

@@ -23,18 +23,15 @@
 #define NT_ITEM 4096            // elements of an item of the kernels that write
 #define NT_THREADS 256          // threads of a block of the update
 #define NT_ADAMW_THREADS 512    // threads of a block of AdamW
-#ifndef NT_STEP_LIST
 #define NT_STEP_LIST (5ll << 23)   // elements from which its blocks are kept in step: one block of a CU, many launches
-#endif
 #define NT_STEP_THREADS 1024    // then: an item in one sweep,
 #define NT_STEP_LDS 82000       // more than half of a CU's LDS, so that one block fits,
 #define NT_STEP_ITEMS 16384     // items of a launch
 #define NT_NORM_THREADS 256     // threads of a block of the norm's kernel
 #define NT_NORM_FLIGHT 4        // 16-byte loads that a thread of it has in flight
 #define NT_LONG_ITEM 8192       // elements of its items in a long list
-#ifndef NT_LONG_BLOCKS
 #define NT_LONG_BLOCKS 1024     // and its blocks, which walk such a list
-#endif
+#define NT_RUN 2                // items of a block in a long list of many groups
 #define NT_LONG_LIST (1ll << 23)   // elements from which a list is long
 #define NT_MOST_BLOCKS (1u << 20)  // blocks of one launch
 // Elements from which loads (and stores) go past the 256 MB cache that the chip's memory has, because what they touch would not stay in it
@@ -43,6 +40,8 @@
 #define NT_STREAM_UPDATE (3ll << 23)   // what an update writes
 #define NT_STREAM_ADAMW (1ll << 23)    // weights and moments
 #define NT_PLAN_MAGIC 0x4e54504cu
+#define NT_PLAN_ROWS 1u         // most elements are in tensors with rows
+#define NT_FEW_SLOTS 1024       // partials of a group that the last block adds up by itself
 #define NT_COUNTER_WORDS 16     // a counter has 64 bytes of its own, so that counting blocks of different slabs do not meet
 
 namespace {
@@ -74,9 +73,9 @@ struct Item {
 __device__ inline Item item_at(const Item* items, uint32_t i) {
   return __builtin_bit_cast(Item, ((const u32x4 NT_CONST*)(uintptr_t)items)[i]);
 }
-// A group's items are consecutive, and so are the partials (slots) that the blocks leave for it.  Block b of the norm's kernel walks items
-// b, b + blocks, ...: it meets a group whose items begin at item0 first at the item that is ((b - item0) mod blocks) further on, and
-// that number is its slot in the group.  A slab is a power of two of a group's slots.
+// A group's items are consecutive, and so are the partials (slots) that the blocks leave for it.  A block that takes a run of items is
+// the (b - item0 / run)-th to meet a group whose items begin at item0.  One that walks items b, b + blocks, ... meets it first at the item that is
+// ((b - item0) mod blocks) further on.  That number is its slot in the group.  A slab is a power of two of a group's slots.
 struct Group {
   uint32_t item0, slot0, slots, slab0;
   int64_t elements, pad;
@@ -94,17 +93,24 @@ struct Cut {
   double* partials;     // one per slot
   double* sums;         // one per slab
   uint32_t nitems, nslabs;
-  uint32_t blocks;      // a power of two
+  uint32_t blocks;      // a power of two: block b takes items b, b + blocks, ...
+  uint32_t run;         // or, if not zero: items b run .. b run + run - 1
   int shift;            // a slab is up to 1 << shift slots
 };
 struct Layout {
   size_t shapes, items[2], groups[2], counters[2], upload, partials[2], sums[2], bytes;
 };
-// Blocks that take a cut's items, which for the first cut is a block for each.  The norm's kernel walks a long list with few, unless its
-// groups are so short that a block would meet another one, and end a part, with almost every item.
-uint32_t blocks_of(const nt_plan& p, int k) {
-  if (k == 0) return 1u << 31;
-  return p.items[1] >= (int64_t)p.groups * 4 * NT_LONG_BLOCKS ? NT_LONG_BLOCKS : 1u << 23;
+// Who takes a cut's items: of the first cut, a block each.  The norm's kernel walks a long list with few blocks, unless its groups are so
+// short that a block would meet another one, and end a part, with almost every item: then a block takes a run of items.
+uint32_t run_of(const nt_plan& p, int k) {
+  if (k == 0) return 1;
+  if (p.items[1] >= (int64_t)p.groups * 4 * NT_LONG_BLOCKS) return 0;
+  return NT_RUN;
+}
+// parts of a group that begins with item `begin`
+int64_t slots_of(uint32_t run, int64_t begin, int64_t items) {
+  if (run) return (begin + items - 1) / run - begin / run + 1;
+  return items < NT_LONG_BLOCKS ? items : NT_LONG_BLOCKS;
 }
 constexpr int64_t SIZES[2] = {NT_ITEM, NT_LONG_ITEM};
 // A slab is all slots, or about as many as there are slabs, so that neither counter is counted up often: a counter takes some 10 ns
@@ -229,6 +235,11 @@ struct Walk {
       col0 = (int64_t)it.idx * size;
       rows = 1;
       width = it.count;
+      quads = size;   // more than there are: no other row follows
+      r = dr = 0;
+      c = threadIdx.x;
+      dc = THREADS;
+      return;
     }
     quads = (width + 3) / 4;
     r = threadIdx.x / quads;
@@ -238,8 +249,8 @@ struct Walk {
   }
   // how many elements there are at this place: 0 past the item's end
   __device__ inline int here() const {
-    const uint32_t left = width - 4 * c;
-    return r < rows ? (int)(left < 4 ? left : 4) : 0;
+    const int left = (int)width - 4 * (int)c;
+    return r < rows && left > 0 ? (left < 4 ? left : 4) : 0;
   }
   __device__ inline void step() {
     r += dr;
@@ -359,31 +370,36 @@ __device__ inline void write_norm(const NormOut& o, uint32_t group, int64_t elem
   o.norms[group] = r;
 }
 
-// The value goes through this XCD's L2 to memory and the count follows it.  Both are relaxed on purpose, since a release would write
-// back all of the L2 in every block: on gfx950 a store of agent scope is written through, s_waitcnt vmcnt(0) returns once it has reached
-// the memory that all XCDs share, and the same wave counts behind it.  The last one's acquire drops what its caches hold.  Nobody waits
-// for another block.  True in the whole wave for the last of n.
+// A value that another block will read goes through this XCD's L2 to memory, and the count follows it.  Both are relaxed on purpose, since
+// a release would write back all of the L2 in every block: on gfx950 a store of agent scope is written through, s_waitcnt vmcnt(0) returns
+// once it has reached the memory that all XCDs share, and the same wave counts behind it.  The last one's acquire drops what its caches hold.
+// Nobody waits for another block.
 template <class T>
-__device__ inline bool last_of(T value, double* to, uint32_t* counter, uint32_t n) {
-  uint32_t before = 0;
+__device__ inline void hand_over(T value, double* to) {
   if ((threadIdx.x & 63) == 0) {
     __hip_atomic_store((uint64_t*)to, __builtin_bit_cast(uint64_t, value), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
+}
+// Counts; true in the whole wave for the last of n, which puts the counter back.
+__device__ inline bool last_of(uint32_t* counter, uint32_t n) {
+  uint32_t before = 0;
+  if ((threadIdx.x & 63) == 0) before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if ((uint32_t)__builtin_amdgcn_readfirstlane((int)before) != n - 1) return false;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   if ((threadIdx.x & 63) == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return true;
 }
-// total of n stored values, in the whole wave
+// total of n values that were handed over, in the whole wave
 template <class K>
 __device__ inline typename K::T total_of(const double* from, uint32_t n) {
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   typename K::T t = 0;
+#pragma unroll 4
   for (uint32_t i = threadIdx.x & 63; i < n; i += 64) t = K::join(t, __builtin_bit_cast(typename K::T, from[i]));
   return wave_total<K>(t);
 }
-// A block's part of group g, which its lanes hold: stored in its slot, counted, and added up by whoever comes last.  A block that meets
+// A block's part of group g, which its lanes hold: stored in its slot, counted, and added up by whoever comes last.  Few slots are counted in
+// slabs but added up at once: 1M elements 6.4 -> 6.0 us, as a slab's sum costs another trip to memory and back.  A block that meets
 // several groups alternates `half`, so that the first wave has read one half before another wave writes it again.
 template <class K, int THREADS>
 __device__ inline void end_part(const NormOut& o, uint32_t block, uint32_t g, typename K::T acc, int half = 0) {
@@ -397,16 +413,23 @@ __device__ inline void end_part(const NormOut& o, uint32_t block, uint32_t g, ty
   for (int w = 1; w < THREADS / 64; ++w) total = K::join(total, red[half][w]);
   const Group NT_CONST* group = constant(o.cut.groups) + g;
   const uint32_t slot0 = group->slot0, slots = group->slots, slab0 = group->slab0;
-  const uint32_t slot = (block - group->item0) & (o.cut.blocks - 1), slab = slot >> o.cut.shift;
-  const uint32_t slabs = ((slots - 1) >> o.cut.shift) + 1, first = slab << o.cut.shift;
-  const uint32_t here = slots - first < (1u << o.cut.shift) ? slots - first : 1u << o.cut.shift;
-  if (here > 1) {
-    if (!last_of(total, o.cut.partials + slot0 + slot, o.cut.counters + (size_t)NT_COUNTER_WORDS * (slab0 + slab), here)) return;
-    total = total_of<K>(o.cut.partials + slot0 + first, here);
-  }
-  if (slabs > 1) {
-    if (!last_of(total, o.cut.sums + slab0 + slab, o.cut.counters + (size_t)NT_COUNTER_WORDS * (o.cut.nslabs + g), slabs)) return;
-    total = total_of<K>(o.cut.sums + slab0, slabs);
+  if (slots > 1) {
+    const uint32_t slot = o.cut.run ? block - group->item0 / o.cut.run : (block - group->item0) & (o.cut.blocks - 1);
+    const uint32_t slab = slot >> o.cut.shift;
+    const uint32_t slabs = ((slots - 1) >> o.cut.shift) + 1, first = slab << o.cut.shift;
+    const uint32_t here = slots - first < (1u << o.cut.shift) ? slots - first : 1u << o.cut.shift;
+    uint32_t* const counters = o.cut.counters;
+    hand_over(total, o.cut.partials + slot0 + slot);
+    if (here > 1 && !last_of(counters + (size_t)NT_COUNTER_WORDS * (slab0 + slab), here)) return;
+    uint32_t* const of_group = counters + (size_t)NT_COUNTER_WORDS * (o.cut.nslabs + g);
+    if (slots <= NT_FEW_SLOTS) {
+      if (slabs > 1 && !last_of(of_group, slabs)) return;
+      total = total_of<K>(o.cut.partials + slot0, slots);
+    } else {
+      hand_over(total_of<K>(o.cut.partials + slot0 + first, here), o.cut.sums + slab0 + slab);
+      if (!last_of(of_group, slabs)) return;
+      total = total_of<K>(o.cut.sums + slab0, slabs);
+    }
   }
   if (threadIdx.x == 0) write_norm<K>(o, g, group->elements, total);
 }
@@ -537,12 +560,14 @@ __device__ inline void norm_rows(const nt_tensor NT_CONST* t, const Item& it, co
     }
   }
 }
-// A block walks every blocks-th item: the chip as a whole reads a long list from front to back, and neither the way to an item's address
+// A block that walks every blocks-th item: the chip as a whole reads a long list from front to back, and neither the way to an item's address
 // nor the end of a part is met more often than need be.  The next item's record and address are fetched beside this one's elements.
 template <class K, bool STREAM>
 __global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_tensor* list, int level, NormOut o) {
   const uint32_t size = level ? NT_LONG_ITEM : NT_ITEM;
-  uint32_t item = blockIdx.x;
+  const uint32_t step = o.cut.run ? 1 : o.cut.blocks;
+  uint32_t item = o.cut.run ? blockIdx.x * o.cut.run : blockIdx.x;
+  const uint32_t end = o.cut.run && o.cut.nitems - item > o.cut.run ? item + o.cut.run : o.cut.nitems;
   Item it = item_at(a.items, item);
   const nt_tensor NT_CONST* t = constant(list) + it.tensor;
   const char NT_GLOBAL* data = nullptr;
@@ -553,8 +578,8 @@ __global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_t
   }
   typename K::T acc = 0;
   for (;;) {
-    const uint32_t next = item + o.cut.blocks;
-    const bool more = next < o.cut.nitems;
+    const uint32_t next = item + step;
+    const bool more = next < end;
     const Item nx = item_at(a.items, more ? next : item);
     const nt_tensor NT_CONST* nt = constant(list) + nx.tensor;
     const char NT_GLOBAL* const from = data + ((uint64_t)it.idx * size << size_shift(dtype));
@@ -867,7 +892,7 @@ Pieces pieces_of(int64_t rows, int64_t cols, int64_t size) {
 Cut cut_of(const nt_plan& p, const Layout& l, int k) {
   char* const b = (char*)p.image;
   return {(const Item*)(b + l.items[k]), (const Group*)(b + l.groups[k]), (uint32_t*)(b + l.counters[k]), (double*)(b + l.partials[k]),
-          (double*)(b + l.sums[k]), p.items[k], p.slabs[k], blocks_of(p, k), slab_shift(p.slots[k])};
+          (double*)(b + l.sums[k]), p.items[k], p.slabs[k], NT_LONG_BLOCKS, run_of(p, k), slab_shift(p.slots[k])};
 }
 
 int check_plan(const nt_plan* p) {
@@ -923,7 +948,7 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
   if (!plan || N < 0 || G < 1 || (N > 0 && !tensors) || misaligned8(image)) return NT_ERR_BAD_ARG;
   nt_plan p;
   std::memset(&p, 0, sizeof(p));
-  int64_t elements = 0;
+  int64_t elements = 0, in_rows = 0;
   for (int32_t i = 0; i < N; ++i) {
     const nt_tensor& t = tensors[i];
     if (t.rows < 0 || t.cols < 0 || t.group < 0 || t.group >= G) return NT_ERR_BAD_ARG;
@@ -931,8 +956,10 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
     int64_t n;
     if (__builtin_mul_overflow(t.rows, t.cols, &n) || __builtin_add_overflow(elements, n, &elements) || elements > (1ll << 43))
       return NT_ERR_TOO_LARGE;
+    if (t.rows > 1) in_rows += n;
   }
   p.elements = elements;
+  p.flags = in_rows > elements / 2 ? NT_PLAN_ROWS : 0;
   p.tensors = N;
   p.groups = G;
   p.magic = NT_PLAN_MAGIC;
@@ -961,7 +988,6 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
     for (int64_t j = group_begin(g); j < first[g]; ++j) n += pieces_of(tensors[order[j]].rows, tensors[order[j]].cols, SIZES[k]).n;
     return n ? n : 1;
   };
-  auto slots_of = [&](int64_t items, int k) { return items < blocks_of(p, k) ? items : (int64_t)blocks_of(p, k); };
   for (int k = 0; k < cuts; ++k) {
     int64_t items = 0, slots = 0, slabs = 0;
     for (int32_t g = 0; g < G; ++g) {
@@ -969,9 +995,9 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
       if (items > (1ll << 31) - 1) return NT_ERR_TOO_LARGE;
     }
     p.items[k] = (uint32_t)items;
-    for (int32_t g = 0; g < G; ++g) slots += slots_of(items_of(g, k), k);
+    for (int32_t g = 0, at = 0; g < G; at += items_of(g, k), ++g) slots += slots_of(run_of(p, k), at, items_of(g, k));
     const int shift = slab_shift((uint32_t)slots);
-    for (int32_t g = 0; g < G; ++g) slabs += ceil_div(slots_of(items_of(g, k), k), 1ll << shift);
+    for (int32_t g = 0, at = 0; g < G; at += items_of(g, k), ++g) slabs += ceil_div(slots_of(run_of(p, k), at, items_of(g, k)), 1ll << shift);
     p.slots[k] = (uint32_t)slots;
     p.slabs[k] = (uint32_t)slabs;
   }
@@ -1014,7 +1040,7 @@ int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* 
           }
         }
         if (item == begin) items[item++] = {0, 0, (uint32_t)g, 0};
-        const uint32_t slots = (uint32_t)slots_of(item - begin, k);
+        const uint32_t slots = (uint32_t)slots_of(run_of(p, k), begin, item - begin);
         groups[g] = {begin, slot, slots, slab, held_elements, 0};
         slot += slots;
         slab += (uint32_t)ceil_div(slots, 1ll << shift);
@@ -1048,7 +1074,7 @@ int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind
   const int k = plan->items[1] ? 1 : 0;
   const NormOut o = {cut_of(*plan, l, k), max_norm, grad_scale, norms};
   const ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), o.cut.items, 0};
-  const uint32_t blocks = o.cut.nitems < o.cut.blocks ? o.cut.nitems : o.cut.blocks;
+  const uint32_t blocks = o.cut.run ? (o.cut.nitems - 1) / o.cut.run + 1 : o.cut.nitems < o.cut.blocks ? o.cut.nitems : o.cut.blocks;
   const bool stream = plan->elements >= NT_STREAM_READ;
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT_NORM_THREADS), 0, (hipStream_t)hip_stream, a, grads, k, o);
@@ -1110,14 +1136,16 @@ int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt
   const Cut cut = cut_of(*plan, l, 0);
   ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), cut.items, 0};
   hipStream_t st = (hipStream_t)hip_stream;
-  const bool step = plan->elements >= NT_STEP_LIST;
+  const bool step = plan->elements >= NT_STEP_LIST && !(plan->flags & NT_PLAN_ROWS);
   return in_launches(plan->items[0], step ? NT_STEP_ITEMS : NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
     auto launch = [&](auto kernel, int threads, int lds) { hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), lds, st, a, u); };
     if (plan->elements < NT_STREAM_ADAMW)
       launch(k_adamw<KEEP, NT_ADAMW_THREADS>, NT_ADAMW_THREADS, 0);
-    else if (!step)
+    else if (!step && plan->elements < NT_STREAM_READ)
       launch(k_adamw<STREAM_WRITTEN, NT_ADAMW_THREADS>, NT_ADAMW_THREADS, 0);
+    else if (!step)
+      launch(k_adamw<STREAM_ALL, NT_ADAMW_THREADS>, NT_ADAMW_THREADS, 0);
     else if (plan->elements < NT_STREAM_READ)
       launch(k_adamw<STREAM_WRITTEN, NT_STEP_THREADS>, NT_STEP_THREADS, NT_STEP_LDS);
     else

@@ -122,14 +122,15 @@ def test_slots_and_slabs_are_a_groups_own(seed):
     _, cuts = cuts_of(plan, image)
     assert len(cuts) == (2 if plan.elements >= 1 << 23 else 1)
     for k, (items, grps, _) in enumerate(cuts):
-        blocks = [1 << 31, 1024 if plan.items[1] >= 4096 * G else 1 << 23][k]
+        run = [1, 0 if plan.items[1] >= 4096 * G else 2][k]
         shift = slab_shift(plan.slots[k])
         assert (np.diff(items["group"].astype(np.int64)) >= 0).all() and set(items["group"]) == set(range(G))
         parts = {}   # group -> slots in the order of their blocks
-        for b in range(min(blocks, len(items))):
-            mine = items["group"][b::blocks] if blocks < len(items) else items["group"][b:b + 1]
+        for b in range(-(-len(items) // run) if run else min(1024, len(items))):
+            mine = items["group"][b * run:(b + 1) * run] if run else items["group"][b::1024]
             for g in np.unique(mine):
-                parts.setdefault(int(g), []).append((b - int(grps["item0"][g])) % blocks)
+                item0 = int(grps["item0"][g])
+                parts.setdefault(int(g), []).append(b - item0 // run if run else (b - item0) % 1024)
         slot0 = slab0 = 0
         for g in range(G):
             assert grps["elements"][g] == sum(r * c for (r, c), h in zip(shapes, groups) if h == g)
