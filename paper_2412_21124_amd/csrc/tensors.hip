@@ -220,8 +220,18 @@ struct Walk {
   uint32_t rows, width, quads;        // of the item
   uint32_t r, c, dr, dc;
   bool wrapped;
-  __device__ inline Walk() {}
-  __device__ inline Walk(const Item& it, const Shape* shapes, int level, uint32_t size) {
+  // `width` elements of a tensor of one row from column `col` on
+  __device__ inline Walk(int64_t col, uint32_t n) {
+    row0 = 0;
+    col0 = col;
+    rows = 1;
+    width = n;
+    quads = 1u << 30;   // more than there are: no other row follows
+    r = dr = 0;
+    c = threadIdx.x;
+    dc = THREADS;
+  }
+  __device__ inline Walk(const Item& it, const Shape* shapes, int level, uint32_t size) : Walk((int64_t)it.idx * size, it.count) {
     if (it.count & NT_ROWS) {
       const Shape NT_CONST* s = constant(shapes) + it.tensor;
       const uint32_t per_row = s->per_row[level];
@@ -230,22 +240,12 @@ struct Walk {
       rows = it.count & ~NT_ROWS;
       const int64_t left = s->cols - col0;
       width = left < size ? (uint32_t)left : size;
-    } else {
-      row0 = 0;
-      col0 = (int64_t)it.idx * size;
-      rows = 1;
-      width = it.count;
-      quads = size;   // more than there are: no other row follows
-      r = dr = 0;
-      c = threadIdx.x;
-      dc = THREADS;
-      return;
+      quads = (width + 3) / 4;
+      r = threadIdx.x / quads;
+      c = threadIdx.x % quads;
+      dr = THREADS / quads;
+      dc = THREADS % quads;
     }
-    quads = (width + 3) / 4;
-    r = threadIdx.x / quads;
-    c = threadIdx.x % quads;
-    dr = THREADS / quads;
-    dc = THREADS % quads;
   }
   // how many elements there are at this place: 0 past the item's end
   __device__ inline int here() const {
@@ -788,9 +788,8 @@ __device__ inline void adamw_flat(const AdamwArgs& u, const char NT_GLOBAL* gp, 
 // Any other item.
 template <int GT, int THREADS>
 __device__ inline void adamw_walk(const AdamwArgs& u, const nt_tensor NT_CONST* gt, const nt_tensor NT_CONST* wt, const nt_tensor NT_CONST* mt,
-                                  const nt_tensor NT_CONST* vt, const nt_tensor NT_CONST* ct, const Item& it, const Shape* shapes, float scale) {
+                                  const nt_tensor NT_CONST* vt, const nt_tensor NT_CONST* ct, Walk<THREADS> at, float scale) {
   constexpr int SWEEPS = NT_ITEM / (4 * THREADS);
-  Walk<THREADS> at(it, shapes, 0, NT_ITEM);
   Place<GT> gp(gt, at);
   Place<NT_F32> wp(wt, at), mp(mt, at), vp(vt, at);
   u32x4 gr[SWEEPS], wr[SWEEPS], mr[SWEEPS], vr[SWEEPS];
@@ -856,17 +855,34 @@ __global__ __launch_bounds__(THREADS) void k_adamw(ListArgs a, AdamwArgs u) {
     scale = (float)u.grad_scale * n->factor;
   }
   const int dtype = gt->dtype;
-  if (it.count == NT_ITEM) {
-    const uint64_t at = (uint64_t)it.idx * NT_ITEM;
-    const int copy_type = ct ? ct->dtype : 0;
-    const char NT_GLOBAL* gp = (const char NT_GLOBAL*)gt->data + (at << size_shift(dtype));
-    char NT_GLOBAL* cp = ct ? (char NT_GLOBAL*)ct->data + (at << size_shift(copy_type)) : nullptr;
+  if (it.count & NT_ROWS) {
     by_type(dtype, [&](auto d) {
-      adamw_flat<decltype(d)::value, STREAM, THREADS>(u, gp, (char NT_GLOBAL*)wt->data + 4 * at, (char NT_GLOBAL*)mt->data + 4 * at,
-                                             (char NT_GLOBAL*)vt->data + 4 * at, cp, copy_type, scale);
+      adamw_walk<decltype(d)::value, THREADS>(u, gt, wt, mt, vt, ct, Walk<THREADS>(it, a.shapes, 0, NT_ITEM), scale);
     });
-  } else {
-    by_type(dtype, [&](auto d) { adamw_walk<decltype(d)::value, THREADS>(u, gt, wt, mt, vt, ct, it, a.shapes, scale); });
+    return;
+  }
+  // In lists that stream, items begin where w has a whole line of memory, and what lies before the first one's begin goes with it: tensors one
+  // right behind the other, 137.5M elements 757 -> 714 us.  In short lists it costs more than it gives (1M elements 12.7 -> 13.5).
+  const int64_t n = wt->cols;
+  const uint32_t ahead = STREAM != KEEP && n > NT_ITEM ? (0u - (uint32_t)((uintptr_t)wt->data >> 2)) % 32 : 0;
+  const int64_t begin = (int64_t)it.idx * NT_ITEM + ahead;
+  const int64_t count = n - begin < NT_ITEM ? n - begin : NT_ITEM;
+  for (bool before = STREAM != KEEP && it.idx == 0 && ahead > 0;; before = false) {
+    if (before || count < NT_ITEM) {
+      if (before || count > 0)
+        by_type(dtype, [&](auto d) {
+          adamw_walk<decltype(d)::value, THREADS>(u, gt, wt, mt, vt, ct, Walk<THREADS>(before ? 0 : begin, before ? ahead : (uint32_t)count), scale);
+        });
+    } else {
+      const int copy_type = ct ? ct->dtype : 0;
+      const char NT_GLOBAL* gp = (const char NT_GLOBAL*)gt->data + (begin << size_shift(dtype));
+      char NT_GLOBAL* cp = ct ? (char NT_GLOBAL*)ct->data + (begin << size_shift(copy_type)) : nullptr;
+      by_type(dtype, [&](auto d) {
+        adamw_flat<decltype(d)::value, STREAM, THREADS>(u, gp, (char NT_GLOBAL*)wt->data + 4 * begin, (char NT_GLOBAL*)mt->data + 4 * begin,
+                                                       (char NT_GLOBAL*)vt->data + 4 * begin, cp, copy_type, scale);
+      });
+    }
+    if (!before) break;
   }
 }
 

@@ -323,6 +323,79 @@ def test_long_lists():
     y_untouched()
 
 
+def pieces(tensors, most=3_000_017):
+    """The tensors cut into short ones (rows are cut between rows)."""
+    out = []
+    for t in tensors:
+        out += t.split(max(1, most // t.shape[1])) if t.dim() == 2 else t.split(most)
+    return out
+
+
+LONG = [
+    # total elements past each length at which a kernel or its memory accesses change, at odd offsets
+    [(8_500_003,), (4097,), (31,)], [(20_000_001,), (5_300_000,), (2,)], [(30_000_001,), (12_000_007,), (2000,)],
+    [(100_000_001,), (34_300_007,), (4096,), (5,)],
+    # most of it in rows, whole and split ones, with ends of one to three elements
+    [(9001, 1001), (3,)], [(4001, 5003), (1000, 9001), (12_345,)], [(20_001, 7003), (5,)],
+]
+
+
+@pytest.mark.parametrize("shapes", LONG, ids=str)
+def test_long_lists_have_the_bits_of_short_ones(shapes):
+    """What is written does not depend on how a list is cut: every call on a long list against calls on short pieces of a copy."""
+    types = cycle((BF16, F32, F16), shapes)
+
+    def lists(tensors, like=None):
+        return B.make_tensor_list(tensors, like=like)
+    results = []
+    for cut in (lambda ts: ts, pieces):
+        x, x_check = carve(shapes, types, 60, offset=1, extra=3)
+        (w, m, v), checks = state(shapes, extra=2)
+        c, c_check = carve(shapes, [BF16] * len(shapes), 61, offset=1, extra=1)
+        y, y_check = carve(shapes, cycle((F32, BF16), shapes), 62, offset=1)
+        whole = lists(x)
+        norms = B.normtest_grad_norm(whole, max_norm=0.5)
+        for k in (range(1) if cut(x) is x else range(len(pieces(x)))):
+            part = (lambda ts: cut(ts)) if cut(x) is x else (lambda ts: [pieces(ts)[k]])
+            # the record of the whole list's norm holds for each piece, which is a list of one group too
+            g = lists(part(x))
+            gw, gm, gv, gc, gy = (lists(part(ts), g) for ts in (w, m, v, c, y))
+            B.normtest_adamw_tensors(g, gw, gm, gv, hyper(), norms=norms, copy=gc)
+            B.normtest_accumulate(gy, g, beta=0.5, scale=0.25, src_norms=norms)
+            B.normtest_accumulate(gw, gy, beta=0.0, norms=B.make_norms(g))
+            B.normtest_clip_grads(g, norms, out=gm)
+            B.normtest_clip_grads(g, norms)
+        torch.cuda.synchronize()
+        for check in (x_check, *checks, c_check, y_check):
+            check()
+        results.append([*x, *w, *m, *v, *c, *y])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shapes", LONG, ids=str)
+@pytest.mark.parametrize("groups", ["one", "each"])
+def test_norms_of_long_lists(shapes, groups):
+    x, _ = carve(shapes, cycle((BF16, F32, F16), shapes), 70, offset=1, extra=3)
+    ids = list(range(len(x))) if groups == "each" else [0] * len(x)
+    lst = B.make_tensor_list(x, groups=ids)
+    norms, stored = B.make_norms(lst), B.make_norms(lst)
+    y, _ = carve(shapes, [F32] * len(shapes), 71)
+    B.normtest_accumulate(B.make_tensor_list(y, like=lst), lst, beta=0.0, norms=stored)
+    for kind in (B.NT_NORM_L2, B.NT_NORM_MAX):
+        B.normtest_grad_norm(lst, norms, max_norm=1.0, kind=kind)
+        total = [0.0] * (max(ids) + 1)
+        for t, g in zip(x, ids):
+            d = t.double()
+            total[g] = max(total[g], float(d.abs().max())) if kind == B.NT_NORM_MAX else total[g] + float(d.square().sum())
+        for r, n in zip(B.read_norms(norms), total):
+            want = n if kind == B.NT_NORM_MAX else math.sqrt(n)
+            assert abs(r.norm - want) <= 1e-12 * want
+        if kind == B.NT_NORM_L2:
+            for r, n in zip(B.read_norms(stored), total):
+                assert abs(r.norm - math.sqrt(n)) <= 1e-12 * math.sqrt(n)
+
+
 def test_elements_past_32_bits():
     """One tensor of more than 2^32 elements, which takes two launches: its ends, the seam and the total."""
     n = (1 << 32) + 4099
