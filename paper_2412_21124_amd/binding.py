@@ -490,10 +490,10 @@ ANY_DTYPE = (1 << NT_F32) | (1 << NT_BF16) | (1 << NT_F16)
 def _rows_of(t: torch.Tensor):
     """(rows, columns, row stride, order) of a tensor in memory: one row where its elements are dense.  order names its dimensions from
     the outermost in memory on, None where that is their own order: only then do elements of tensors of other shapes correspond."""
-    dims = [i for i in range(t.dim()) if t.shape[i] != 1]
     n = t.numel()
-    if n == 0 or not dims:
+    if t.is_contiguous():
         return 1, n, n, None
+    dims = [i for i in range(t.dim()) if t.shape[i] != 1]
     by_stride = sorted(dims, key=lambda i: -t.stride(i))
     order = None if by_stride == dims else tuple(by_stride)
     merged = []   # (size, stride) from the innermost out
@@ -516,13 +516,14 @@ class TensorPlan:
     """How the tensors of a list are cut into pieces, on the device, with the scratch memory of its norms.  Made by make_tensor_list
     and shared by the lists made `like` it; one call at a time may use it."""
 
-    def __init__(self, records, count: int, orders, shapes, groups: int, device: torch.device):
-        self.records, self.orders, self.shapes, self.groups, self.device = records, orders, shapes, groups, device
+    def __init__(self, records, layouts, groups: int, device: torch.device):
+        # layouts: (rows, columns, order, group, shape) of every tensor
+        self.records, self.layouts, self.groups, self.device = records, layouts, groups, device
         self.record = nt_plan()
-        rc = lib().normtest_plan_make(records, count, groups, ctypes.byref(self.record), None, 0)
+        rc = lib().normtest_plan_make(records, len(layouts), groups, ctypes.byref(self.record), None, 0)
         if rc == NT_OK:
             host = torch.empty(max(8, self.record.upload_bytes), dtype=torch.uint8)
-            rc = lib().normtest_plan_make(records, count, groups, ctypes.byref(self.record), host.data_ptr(), host.numel())
+            rc = lib().normtest_plan_make(records, len(layouts), groups, ctypes.byref(self.record), host.data_ptr(), host.numel())
         if rc != NT_OK:
             raise NormtestError(rc, "normtest_plan_make")
         self.image = torch.empty(max(16, self.record.bytes), dtype=torch.uint8, device=device)
@@ -589,18 +590,17 @@ def _check_listed(tensors, device):
 def _like_records(tensors, plan: TensorPlan):
     """Records of tensors that correspond, element by element in memory, to those the plan was made for."""
     _check_listed(tensors, plan.device)
-    records = (nt_tensor * len(tensors))()
-    for i, t in enumerate(tensors):
-        want, order = plan.records[i], plan.orders[i]
+    made = []
+    for i, (t, (prows, pcols, order, group, shape)) in enumerate(zip(tensors, plan.layouts)):
         rows, cols, ld, own_order = _rows_of(t)
-        same = (rows, cols) == (want.rows, want.cols)
-        if rows == 1 and cols == want.rows * want.cols:   # dense: in the plan's rows
-            rows, cols, ld, same = want.rows, want.cols, want.cols, True
-        if not same or own_order != order or (order is not None and tuple(t.shape) != plan.shapes[i]):
+        same = (rows, cols) == (prows, pcols)
+        if rows == 1 and cols == prows * pcols:   # dense: in the plan's rows
+            rows, cols, ld, same = prows, pcols, pcols, True
+        if not same or own_order != order or (order is not None and t.shape != shape):
             raise ValueError("tensor %d of the list does not lie in memory as the plan's: shape %s, strides %s against %s (make the plan "
-                             "from the list that has row strides)" % (i, tuple(t.shape), t.stride(), plan.shapes[i]))
-        records[i] = nt_tensor(t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], want.group)
-    return records
+                             "from the list that has row strides)" % (i, tuple(t.shape), t.stride(), tuple(shape)))
+        made.append((t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], group))
+    return (nt_tensor * len(made))(*made)
 
 
 def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, like: Optional[TensorList] = None, device=None) -> TensorList:
@@ -631,13 +631,13 @@ def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, lik
     num_groups = max(groups, default=0) + 1 if num_groups is None else int(num_groups)
     if num_groups <= max(groups, default=0):
         raise ValueError("num_groups is %d, but a tensor is in group %d" % (num_groups, max(groups, default=0)))
-    records, orders = (nt_tensor * len(tensors))(), []
-    for i, (t, g) in enumerate(zip(tensors, groups)):
+    made, layouts = [], []
+    for t, g in zip(tensors, groups):
         rows, cols, ld, order = _rows_of(t)
-        records[i] = nt_tensor(t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], g)
-        orders.append(order)
-    plan = TensorPlan(records, len(tensors), orders, [tuple(t.shape) for t in tensors], num_groups, device)
-    return TensorList(tensors, plan, records)
+        made.append((t.data_ptr(), rows, cols, ld, _LIST_DTYPES[t.dtype], g))
+        layouts.append((rows, cols, order, g, t.shape))
+    records = (nt_tensor * len(made))(*made)
+    return TensorList(tensors, TensorPlan(records, layouts, num_groups, device), records)
 
 
 def make_norms(lst: TensorList) -> torch.Tensor:
