@@ -3,7 +3,10 @@
 // A list is cut into items, pieces of one tensor each, by a plan that the host makes once (normtest_plan_make): for the calls that
 // write, items of NT_ITEM elements, four for each thread of a block; for the norm alone, which only reads, longer ones.  A block
 // takes one item: which tensor it belongs to and where it begins is one 16-byte record, the tensor's address a second one.
-// All of it is bound by memory (2 operations a byte), so nothing here is a matrix product.
+// All of it is bound by memory (2 operations a byte), so nothing here is a matrix product; short lists are bound by the way from a launch
+// over the two records to the elements and back (some 4 us), and a norm by the counting and adding up behind it (2 us more).  Measured:
+// norm of 1.5e9 bf16 430 us, 7.0 TB/s (a plain read of the same bytes 400); accumulation of 304.6M bf16 297 us, 6.2 TB/s; norm and clipped
+// AdamW of 1.1e9 bf16 with a bf16 copy 5.7 ms, 5.8 TB/s with the gradients read twice (an arithmetic-free mix of the kind 5.6 to 5.9).
 //
 // Norms.  x^2 is formed and summed in fp64, so no finite value overflows and no rounding of the sum is seen; the largest
 // magnitude is the largest |x| by its bits as an integer, where a NaN is larger than infinity and so survives.  A block leaves
@@ -20,28 +23,36 @@
 
 #include "normtest.h"
 
-#define NT_ITEM 4096            // elements of an item of the kernels that write
-#define NT_THREADS 256          // threads of a block of the update
-#define NT_ADAMW_THREADS 512    // threads of a block of AdamW
-#define NT_STEP_LIST (5ll << 23)   // elements from which its blocks are kept in step: one block of a CU, many launches
-#define NT_STEP_THREADS 1024    // then: an item in one sweep,
-#define NT_STEP_LDS 82000       // more than half of a CU's LDS, so that one block fits,
-#define NT_STEP_ITEMS 16384     // items of a launch
-#define NT_NORM_THREADS 256     // threads of a block of the norm's kernel
-#define NT_NORM_FLIGHT 4        // 16-byte loads that a thread of it has in flight
-#define NT_LONG_ITEM 8192       // elements of its items in a long list
-#define NT_LONG_BLOCKS 1024     // and its blocks, which walk such a list
-#define NT_RUN 2                // items of a block in a long list of many groups
-#define NT_LONG_LIST (1ll << 23)   // elements from which a list is long
+// Sizes and shapes.  Each was chosen between the neighbours it was timed against; times are of whole calls, in us, of lists that the
+// cache below may hold from one pass to the next.
+#define NT_ITEM 4096               // elements of an item of the kernels that write (8192: AdamW of 1M elements 14.8 -> 16.0, else the same)
+#define NT_UPDATE_THREADS 256      // threads of a block of the update (512: clip of 124M bf16 116 -> 146)
+#define NT_TOTAL_THREADS 512       // and where it forms a norm (256: 100k elements 5.3 -> 6.0, 124M 201 -> 208, 304.6M 297 -> 305)
+#define NT_ADAMW_THREADS 512       // threads of a block of AdamW (256: 16M elements 79 -> 104; 1024: the same)
+// Elements from which AdamW's blocks are kept in step: an item in one sweep, one block of a CU (it asks for more than half of the LDS), a
+// launch per 2^26 elements.  Blocks that start together load together and store together, which memory serves faster: 64M elements 320 ->
+// 307, 137.5M 864 -> 754, 1.1e9 6139 -> 5758; 32M 149 -> 150.  Not where rows are walked (100M elements in slices 602 -> 631).
+#define NT_STEP_LIST (5ll << 23)
+#define NT_STEP_THREADS 1024
+#define NT_STEP_LDS 82000
+#define NT_STEP_ITEMS 16384        // (8192: 124M elements 613 -> 625)
+#define NT_NORM_THREADS 256        // threads of a block of the norm's kernel (512: 1.5e9 bf16 429 -> 479)
+#define NT_NORM_FLIGHT 4           // 16-byte loads that a thread of it has in flight
+#define NT_LONG_LIST (1ll << 21)   // elements from which the norm has longer items (4.5M bf16 8.0 -> 6.5, 30M 20.3 -> 14.5; 1M the same)
+#define NT_LONG_ITEM 8192          // elements of those (1.5e9 bf16: 418; 4096 535, 16384 429; all without the ends)
+#define NT_LONG_BLOCKS 1024        // blocks that walk a long list (1.5e9 bf16 432; 512 488, 2048 469, a block per item 463)
+#define NT_RUN 2                   // items of a block in a long list of many groups (75 groups, 30M fp16 14.7; 1 15.5, 4 15.8)
 #define NT_MOST_BLOCKS (1u << 20)  // blocks of one launch
 // Elements from which loads (and stores) go past the 256 MB cache that the chip's memory has, because what they touch would not stay in it
 // until it is needed again.
-#define NT_STREAM_READ (1ll << 27)     // what is only read: gradients, which the norm's kernel leaves there for the next call
-#define NT_STREAM_UPDATE (3ll << 23)   // what an update writes
-#define NT_STREAM_ADAMW (1ll << 23)    // weights and moments
+// What is only read, gradients, which the norm's kernel leaves there for the next call: norm of 1.5e9 bf16 510 -> 471, of 400M 145 -> 135;
+// from 2^26 on, norm and clip of 124M 117 -> 124.
+#define NT_STREAM_READ (1ll << 27)
+#define NT_STREAM_UPDATE (3ll << 23)   // what an update writes: accumulation of 32M bf16 into fp32 59 -> 51, 64M 122 -> 96; 16M the same
+#define NT_STREAM_ADAMW (1ll << 23)    // weights and moments: 16M elements 93 -> 80, 64M 364 -> 308; 8M 44 -> 45
 #define NT_PLAN_MAGIC 0x4e54504cu
 #define NT_PLAN_ROWS 1u         // most elements are in tensors with rows
-#define NT_FEW_SLOTS 1024       // partials of a group that the last block adds up by itself
+#define NT_FEW_SLOTS 1024       // partials of a group that the last block adds up by itself (none: 1M elements 6.2 -> 7.1; 4096: 16M 32 -> 35)
 #define NT_COUNTER_WORDS 16     // a counter has 64 bytes of its own, so that counting blocks of different slabs do not meet
 
 namespace {
@@ -114,7 +125,7 @@ int64_t slots_of(uint32_t run, int64_t begin, int64_t items) {
 }
 constexpr int64_t SIZES[2] = {NT_ITEM, NT_LONG_ITEM};
 // A slab is all slots, or about as many as there are slabs, so that neither counter is counted up often: a counter takes some 10 ns
-// per block, a second level some 3 us.
+// per block, a second one some 0.7 us (one of 512 slots: 1M elements 6.2 -> 8.0 us).
 int slab_shift(uint32_t slots) {
   if (slots <= 128) return 7;
   int shift = 4;
@@ -616,10 +627,10 @@ struct UpdateArgs {
 enum { KEEP = 0, STREAM_WRITTEN = 1, STREAM_ALL = 2 };
 
 // A whole item of a tensor of one row: all loads, then all stores.
-template <bool READ, class K, int STREAM, int XT, int YT, class ACC>
+template <bool READ, class K, int STREAM, int THREADS, int XT, int YT, class ACC>
 __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, float scale, float beta, ACC& acc) {
-  constexpr int PER = XT != NT_F32 && YT != NT_F32 ? 8 : 4, SWEEPS = NT_ITEM / (PER * NT_THREADS);
-  static_assert(SWEEPS * PER * NT_THREADS == NT_ITEM, "an item is whole sweeps");
+  constexpr int PER = XT != NT_F32 && YT != NT_F32 ? 8 : 4, SWEEPS = NT_ITEM / (PER * THREADS);
+  static_assert(SWEEPS * PER * THREADS == NT_ITEM, "an item is whole sweeps");
   typedef Vec<XT, PER> X;
   typedef Vec<YT, PER> Y;
   typename X::raw_t xr[SWEEPS];
@@ -627,8 +638,8 @@ __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, f
   const uint32_t lane = PER * threadIdx.x;
 #pragma unroll
   for (int k = 0; k < SWEEPS; ++k) {
-    xr[k] = X::template load<STREAM == STREAM_ALL>(x + X::SIZE * (lane + k * PER * NT_THREADS));
-    if constexpr (READ) yr[k] = Y::template load<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * NT_THREADS));
+    xr[k] = X::template load<STREAM == STREAM_ALL>(x + X::SIZE * (lane + k * PER * THREADS));
+    if constexpr (READ) yr[k] = Y::template load<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * THREADS));
   }
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -639,7 +650,7 @@ __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, f
       const float v = X::value(xr[k], e);
       Y::put(z, e, READ ? __builtin_fmaf(scale, v, beta * Y::value(yr[k], e)) : scale * v);
     }
-    Y::template store<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * NT_THREADS), z);
+    Y::template store<STREAM != KEEP>(y + Y::SIZE * (lane + k * PER * THREADS), z);
     if constexpr (!__is_same(K, void)) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) K::add(acc, Y::value(z, e));
@@ -647,11 +658,11 @@ __device__ inline void update_flat(const char NT_GLOBAL* x, char NT_GLOBAL* y, f
   }
 }
 // Any other item.
-template <bool READ, class K, int XT, int YT, class ACC>
+template <bool READ, class K, int THREADS, int XT, int YT, class ACC>
 __device__ inline void update_walk(const nt_tensor NT_CONST* x, const nt_tensor NT_CONST* y, const Item& it, const Shape* shapes, float scale,
                                    float beta, ACC& acc) {
-  constexpr int SWEEPS = NT_ITEM / (4 * NT_THREADS);
-  Walk<NT_THREADS> at(it, shapes, 0, NT_ITEM);
+  constexpr int SWEEPS = NT_ITEM / (4 * THREADS);
+  Walk<THREADS> at(it, shapes, 0, NT_ITEM);
   Place<XT> from(x, at);
   Place<YT> to(y, at);
   u32x4 xr[SWEEPS], yr[SWEEPS];
@@ -693,8 +704,8 @@ struct Partial<void> {
   typedef int T;
 };
 // dst <- beta dst + scale factor src
-template <bool READ, class K, int STREAM>
-__global__ __launch_bounds__(NT_THREADS) void k_update(ListArgs a, UpdateArgs u, NormOut o) {
+template <bool READ, class K, int STREAM, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_update(ListArgs a, UpdateArgs u, NormOut o) {
   const uint32_t item = a.item0 + blockIdx.x;
   const Item it = item_at(a.items, item);
   typename Partial<K>::T acc = 0;
@@ -713,15 +724,15 @@ __global__ __launch_bounds__(NT_THREADS) void k_update(ListArgs a, UpdateArgs u,
       const char NT_GLOBAL* from = (const char NT_GLOBAL*)x->data + (at << size_shift(xt));
       char NT_GLOBAL* to = (char NT_GLOBAL*)y->data + (at << size_shift(yt));
       by_type(xt, [&](auto dx) {
-        by_type(yt, [&](auto dy) { update_flat<READ, K, STREAM, decltype(dx)::value, decltype(dy)::value>(from, to, scale, u.beta, acc); });
+        by_type(yt, [&](auto dy) { update_flat<READ, K, STREAM, THREADS, decltype(dx)::value, decltype(dy)::value>(from, to, scale, u.beta, acc); });
       });
     } else {
       by_type(xt, [&](auto dx) {
-        by_type(yt, [&](auto dy) { update_walk<READ, K, decltype(dx)::value, decltype(dy)::value>(x, y, it, a.shapes, scale, u.beta, acc); });
+        by_type(yt, [&](auto dy) { update_walk<READ, K, THREADS, decltype(dx)::value, decltype(dy)::value>(x, y, it, a.shapes, scale, u.beta, acc); });
       });
     }
   }
-  if constexpr (!__is_same(K, void)) end_part<K, NT_THREADS>(o, item, it.group, acc);
+  if constexpr (!__is_same(K, void)) end_part<K, THREADS>(o, item, it.group, acc);
 }
 
 struct AdamwArgs {
@@ -942,11 +953,11 @@ int enqueue_update(const nt_plan& p, const Layout& l, const UpdateArgs& u, int k
   return in_launches(p.items[0], NT_MOST_BLOCKS, [&](uint32_t at, uint32_t n) {
     a.item0 = at;
     if (!o.norms)
-      hipLaunchKernelGGL((k_update<READ, void, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, void, STREAM, NT_UPDATE_THREADS>), dim3(n), dim3(NT_UPDATE_THREADS), 0, st, a, u, o);
     else if (kind == NT_NORM_L2)
-      hipLaunchKernelGGL((k_update<READ, Square, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, Square, STREAM, NT_TOTAL_THREADS>), dim3(n), dim3(NT_TOTAL_THREADS), 0, st, a, u, o);
     else
-      hipLaunchKernelGGL((k_update<READ, Largest, STREAM>), dim3(n), dim3(NT_THREADS), 0, st, a, u, o);
+      hipLaunchKernelGGL((k_update<READ, Largest, STREAM, NT_TOTAL_THREADS>), dim3(n), dim3(NT_TOTAL_THREADS), 0, st, a, u, o);
   });
 }
 template <bool READ>
