@@ -41,7 +41,7 @@
 #define NT_LONG_LIST (1ll << 21)   // elements from which the norm has longer items (4.5M bf16 8.0 -> 6.5, 30M 20.3 -> 14.5; 1M the same)
 #define NT_LONG_ITEM 8192          // elements of those (1.5e9 bf16: 418; 4096 535, 16384 429; all without the ends)
 #define NT_LONG_BLOCKS 1024        // blocks that walk a long list (1.5e9 bf16 432; 512 488, 2048 469, a block per item 463)
-#define NT_RUN 2                   // items of a block in a long list of many groups (75 groups, 30M fp16 14.7; 1 15.5, 4 15.8)
+#define NT_RUN 2                   // items of a block in a long list of many groups (75 groups, 30M fp16 14.7; 1 15.5, 4 15.8; of rows 1: 3M bf16 8.5 -> 7.2)
 #define NT_MOST_BLOCKS (1u << 20)  // blocks of one launch
 // Elements from which loads (and stores) go past the 256 MB cache that the chip's memory has, because what they touch would not stay in it
 // until it is needed again.
@@ -115,8 +115,8 @@ struct Layout {
 // short that a block would meet another one, and end a part, with almost every item: then a block takes a run of items.
 uint32_t run_of(const nt_plan& p, int k) {
   if (k == 0) return 1;
-  if (p.items[1] >= (int64_t)p.groups * 4 * NT_LONG_BLOCKS) return 0;
-  return NT_RUN;
+  if (p.items[1] >= (int64_t)p.groups * NT_LONG_BLOCKS) return 0;
+  return p.flags & NT_PLAN_ROWS ? 1 : NT_RUN;
 }
 // parts of a group that begins with item `begin`
 int64_t slots_of(uint32_t run, int64_t begin, int64_t items) {

@@ -122,7 +122,8 @@ def test_slots_and_slabs_are_a_groups_own(seed):
     _, cuts = cuts_of(plan, image)
     assert len(cuts) == (2 if plan.elements >= 1 << 21 else 1)
     for k, (items, grps, _) in enumerate(cuts):
-        run = [1, 0 if plan.items[1] >= 4096 * G else 2][k]
+        rows = 2 * sum(r * c for r, c in shapes if r > 1) > plan.elements
+        run = [1, 0 if plan.items[1] >= 1024 * G else 1 if rows else 2][k]
         shift = slab_shift(plan.slots[k])
         assert (np.diff(items["group"].astype(np.int64)) >= 0).all() and set(items["group"]) == set(range(G))
         parts = {}   # group -> slots in the order of their blocks
