@@ -19,7 +19,7 @@
  * fp32 state.  Between those limits results are scale-invariant to the stated tolerances.
  *
  * All pointers named "device" must be dereferenceable by the GPU (device memory; result may also be
- * pinned host memory).  The library allocates nothing, keeps nothing of one call for the next
+ * pinned host memory).  The library allocates no device memory, keeps nothing of one call for the next
  * (its launches count their blocks in counters of its own on the device, which every launch leaves at zero; up to 4096 streams
  * are given some of their own, found by the stream's handle, and a short step on any further stream ends in a second kernel), never
  * synchronises the device and never touches host copies of the data: it validates, enqueues kernels
@@ -366,8 +366,8 @@ enum { NT_SKIP_NONFINITE = 1u };   /* leave the tensors of a group alone whose s
 
 /* Fill `plan` for N tensors (host array; N may be 0) in G >= 1 groups, and, if `image` is not NULL, the host image of
  * plan->upload_bytes bytes (8-byte aligned; call once without it to learn the size).  plan->image is left as it is.
- * NT_ERR_BAD_ARG: a negative size, ld < cols where rows > 1, a group outside 0 .. G-1, G < 1 or N < 0;
- * NT_ERR_TOO_LARGE: more than 2^43 elements. */
+ * Host memory that it works in is freed before it returns.  NT_ERR_BAD_ARG: a negative size, ld < cols where rows > 1, a group outside
+ * 0 .. G-1, G < 1 or N < 0; NT_ERR_WORKSPACE_TOO_SMALL: image_bytes < upload_bytes; NT_ERR_TOO_LARGE: more than 2^43 elements. */
 int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* plan, void* image, size_t image_bytes);
 
 /* Host check of a list before it is copied to the device: the shapes are those of `like` (host arrays of N), addresses are there
