@@ -343,17 +343,31 @@ struct Largest {
   __device__ static inline T join(T a, T b) { return a > b ? a : b; }
   __device__ static inline double norm(T a) { return (double)__builtin_bit_cast(float, (uint32_t)a); }
 };
-// the value of lane ^ MASK
-template <class T>
-__device__ inline T across(T x, int mask) {
-  uint64_t w = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = __shfl_xor((int)(uint32_t)w, mask), hi = __shfl_xor((int)(w >> 32), mask);
-  return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
-}
+// Total over the wave, in its first lane, on the vector unit: register halves and then rows of 16 lanes change places, and within a row
+// values move up by 8, 4, 2 and 1 lanes (zeros come in, which add nothing).  By permutes through LDS a norm of 100k elements took 4.6 us instead of 4.3.
+struct Words {
+  uint32_t lo, hi;
+};
 template <class K>
 __device__ inline typename K::T wave_total(typename K::T x) {
-#pragma unroll
-  for (int mask = 32; mask > 0; mask >>= 1) x = K::join(x, across(x, mask));
+  typedef typename K::T T;
+  Words w = __builtin_bit_cast(Words, x);
+  auto lo = __builtin_amdgcn_permlane32_swap(w.lo, w.lo, false, false);
+  auto hi = __builtin_amdgcn_permlane32_swap(w.hi, w.hi, false, false);
+  x = K::join(__builtin_bit_cast(T, (Words{lo[0], hi[0]})), __builtin_bit_cast(T, (Words{lo[1], hi[1]})));
+  w = __builtin_bit_cast(Words, x);
+  lo = __builtin_amdgcn_permlane16_swap(w.lo, w.lo, false, false);
+  hi = __builtin_amdgcn_permlane16_swap(w.hi, w.hi, false, false);
+  x = K::join(__builtin_bit_cast(T, (Words{lo[0], hi[0]})), __builtin_bit_cast(T, (Words{lo[1], hi[1]})));
+#define NT_UP(LANES)                                                                                       \
+  w = __builtin_bit_cast(Words, x);                                                                        \
+  x = K::join(x, __builtin_bit_cast(T, (Words{(uint32_t)__builtin_amdgcn_mov_dpp((int)w.lo, 0x100 + LANES, 0xf, 0xf, true), \
+                                              (uint32_t)__builtin_amdgcn_mov_dpp((int)w.hi, 0x100 + LANES, 0xf, 0xf, true)})))
+  NT_UP(8);
+  NT_UP(4);
+  NT_UP(2);
+  NT_UP(1);
+#undef NT_UP
   return x;
 }
 
@@ -400,7 +414,7 @@ __device__ inline bool last_of(uint32_t* counter, uint32_t n) {
   if ((threadIdx.x & 63) == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return true;
 }
-// total of n values that were handed over, in the whole wave
+// total of n values that were handed over, in the first lane
 template <class K>
 __device__ inline typename K::T total_of(const double* from, uint32_t n) {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
