@@ -605,13 +605,17 @@ __global__ __launch_bounds__(NT_NORM_THREADS) void k_norm(ListArgs a, const nt_t
   for (;;) {
     const uint32_t next = item + step;
     const bool more = next < end;
-    const Item nx = item_at(a.items, more ? next : item);
-    const nt_tensor NT_CONST* nt = constant(list) + nx.tensor;
     const char NT_GLOBAL* const from = data + ((uint64_t)it.idx * size << size_shift(dtype));
     const int type = dtype;
-    if (nx.count) {
-      data = (const char NT_GLOBAL*)nt->data;
-      dtype = nt->dtype;
+    Item nx = it;
+    const nt_tensor NT_CONST* nt = t;
+    if (more) {
+      nx = item_at(a.items, next);
+      nt = constant(list) + nx.tensor;
+      if (nx.count) {
+        data = (const char NT_GLOBAL*)nt->data;
+        dtype = nt->dtype;
+      }
     }
     if (it.count & NT_ROWS)
       by_type(type, [&](auto d) { norm_rows<K, decltype(d)::value>(t, it, a.shapes, level, size, acc); });
