@@ -4,9 +4,9 @@
 // write, items of NT_ITEM elements, four for each thread of a block; for the norm alone, which only reads, longer ones.  A block
 // takes one item: which tensor it belongs to and where it begins is one 16-byte record, the tensor's address a second one.
 // All of it is bound by memory (2 operations a byte), so nothing here is a matrix product; short lists are bound by the way from a launch
-// over the two records to the elements and back (some 4 us), and a norm by the counting and adding up behind it (2 us more).  Measured:
-// norm of 1.5e9 bf16 430 us, 7.0 TB/s (a plain read of the same bytes 400); accumulation of 304.6M bf16 297 us, 6.2 TB/s; norm and clipped
-// AdamW of 1.1e9 bf16 with a bf16 copy 5.7 ms, 5.8 TB/s with the gradients read twice (an arithmetic-free mix of the kind 5.6 to 5.9).
+// over the two records to the elements and back (some 4 us), and a norm by the counting and adding up behind it (1 to 2 us more).  Measured:
+// norm of 1.5e9 bf16 432 us, 6.9 TB/s (a plain read of the same bytes 400); accumulation of 304.6M bf16 291 us, 6.3 TB/s; norm and clipped
+// AdamW of 1.1e9 bf16 with a bf16 copy 5.6 ms, 5.9 TB/s with the gradients read twice (an arithmetic-free mix of the kind 5.6 to 5.9).
 //
 // Norms.  x^2 is formed and summed in fp64, so no finite value overflows and no rounding of the sum is seen; the largest
 // magnitude is the largest |x| by its bits as an integer, where a NaN is larger than infinity and so survives.  A block leaves
@@ -424,7 +424,7 @@ __device__ inline typename K::T total_of(const double* from, uint32_t n) {
   return wave_total<K>(t);
 }
 // A block's part of group g, which its lanes hold: stored in its slot, counted, and added up by whoever comes last.  Few slots are counted in
-// slabs but added up at once: 1M elements 6.4 -> 6.0 us, as a slab's sum costs another trip to memory and back.  A block that meets
+// slabs but added up at once: 1M elements 7.1 -> 6.2 us, as a slab's sum costs another trip to memory and back.  A block that meets
 // several groups alternates `half`, so that the first wave has read one half before another wave writes it again.
 template <class K, int THREADS>
 __device__ inline void end_part(const NormOut& o, uint32_t block, uint32_t g, typename K::T acc, int half = 0) {
