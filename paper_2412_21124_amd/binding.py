@@ -645,6 +645,18 @@ def make_norms(lst: TensorList) -> torch.Tensor:
     return torch.zeros(lst.plan.groups * NORM_BYTES, dtype=torch.uint8, device=lst.plan.device)
 
 
+def _norms_for(lst: TensorList, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """make_norms for a call that writes every record.  On another stream than the current one they are that stream's memory: memory of the
+    current stream could still be written by what runs there.  The caller may read them on either."""
+    size, dev = lst.plan.groups * NORM_BYTES, lst.plan.device
+    if _stream_handle(stream, dev) == _stream_handle(None, dev):
+        return torch.empty(size, dtype=torch.uint8, device=dev)
+    with torch.cuda.stream(stream):
+        norms = torch.empty(size, dtype=torch.uint8, device=dev)
+    norms.record_stream(torch.cuda.current_stream(dev))
+    return norms
+
+
 def norm_views(norms: torch.Tensor) -> dict:
     """Views of the records on the device, one entry per group: norm, factor (float32), flags (int32: status, clipped)."""
     words = NORM_BYTES // 4
@@ -703,7 +715,7 @@ def normtest_grad_norm(grads: TensorList, norms: Optional[torch.Tensor] = None, 
             return norms
     plan = _first("normtest_grad_norm", grads)
     if norms is None:
-        norms = make_norms(grads)
+        norms = _norms_for(grads, stream)
     _list_call("normtest_grad_norm", plan, (grads,), (norms,), stream, lib().normtest_grad_norm, grads.table.data_ptr(), kind, float(max_norm),
                float(grad_scale), norms.data_ptr())
     return norms

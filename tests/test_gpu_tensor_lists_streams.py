@@ -1,0 +1,32 @@
+"""Calls on lists on other streams than the current one, while that one is busy."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+from paper_2412_21124_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BUSY = 200_000_000   # cycles: about a tenth of a second
+
+
+def test_records_made_for_a_call_on_another_stream():
+    """The call is ordered behind what the current stream had to do before it, and nothing of its own is left to the current stream."""
+    x = torch.full((100_000,), 2.0, device=DEV)
+    lst = B.make_tensor_list([x])
+    norm = 2.0 * math.sqrt(x.numel())
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        x.fill_(2.0)
+        side.wait_stream(torch.cuda.current_stream())
+        torch.cuda._sleep(BUSY)
+        records = B.normtest_clip_grad_norm(lst, 1.0, stream=side)
+        side.synchronize()
+        assert not torch.cuda.current_stream().query()   # busy to the end
+        torch.cuda.synchronize()
+        r = B.read_norms(records)[0]
+        assert abs(r.norm - norm) <= 1e-12 * norm and r.clipped and r.elements == x.numel()
+        assert bool(((x - 2.0 / norm).abs() <= 1e-6 * 2.0 / norm).all())
