@@ -550,12 +550,13 @@ class TensorList:
         host = torch.frombuffer(bytearray(self._records), dtype=torch.uint8) if n else torch.zeros(8, dtype=torch.uint8)
         if self.table is None or self.table.numel() != host.numel():
             self.table = torch.empty(host.numel(), dtype=torch.uint8, device=self.plan.device)
+            self.stream = _stream_handle(None, self.plan.device)   # whose memory it is
         self.table.copy_(host)
         self.addresses = [t.data_ptr() for t in self.tensors]
         self.dtypes = {t.dtype for t in self.tensors}
-        # for the native call path; None: its calls are then left to Python
-        self.native = _fast and _fast.make_list(self.tensors, self.addresses, ctypes.addressof(self.plan.record), self.plan.record, self.table,
-                                                self.plan.stream)
+        # for the native call path, which takes calls on the stream that table and plan are memory of; None: its calls are left to Python
+        self.native = _fast and self.stream == self.plan.stream and _fast.make_list(
+            self.tensors, self.addresses, ctypes.addressof(self.plan.record), self.plan.record, self.table, self.stream) or None
 
     def refresh(self, tensors=None) -> "TensorList":
         """Reads the tensors' addresses again, or those of other tensors of the same shapes and layouts (gradients that were allocated
@@ -686,11 +687,12 @@ def _list_call(where: str, plan: TensorPlan, lists, norms, stream, fn, *args):
     rc = _call(plan.device, fn, ctypes.byref(plan.record), *args, st)
     if rc != NT_OK:
         raise NormtestError(rc, where)
-    if st != plan.stream:   # the tables' memory stays until this stream has read them
+    # memory of other streams stays until this one has used it
+    others = [memory for memory, owner in [(plan.image, plan.stream), *[(lst.table, lst.stream) for lst in lists]] if owner != st]
+    if others:
         stream = torch.cuda.current_stream(plan.device) if stream is None else stream
-        plan.image.record_stream(stream)
-        for lst in lists:
-            lst.table.record_stream(stream)
+        for memory in others:
+            memory.record_stream(stream)
 
 
 def _native(lst):

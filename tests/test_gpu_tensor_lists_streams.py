@@ -30,3 +30,21 @@ def test_records_made_for_a_call_on_another_stream():
         r = B.read_norms(records)[0]
         assert abs(r.norm - norm) <= 1e-12 * norm and r.clipped and r.elements == x.numel()
         assert bool(((x - 2.0 / norm).abs() <= 1e-6 * 2.0 / norm).all())
+
+
+def test_a_list_made_on_another_stream_and_dropped():
+    """Its table stays until the call has run, also where the plan was made on the call's stream."""
+    x, y = torch.full((50_000,), 2.0, device=DEV), torch.zeros(50_000, device=DEV)
+    src = B.make_tensor_list([x])
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        dst = B.make_tensor_list([y], like=src)
+    at, size = dst.table.data_ptr(), dst.table.numel()
+    torch.cuda._sleep(BUSY)
+    B.normtest_accumulate(dst, src, beta=0.0, scale=0.5)
+    del dst
+    with torch.cuda.stream(side):
+        given = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(64)]
+    assert not torch.cuda.current_stream().query() and at not in [t.data_ptr() for t in given]
+    torch.cuda.synchronize()
+    assert bool((y == 1.0).all())

@@ -77,3 +77,47 @@ def test_records_made_for_a_call_on_another_stream(streams):
         assert norms.dtype == torch.uint8 and norms.numel() == 2 * B.NORM_BYTES
         assert streams.owner[norms.data_ptr()] == 7 and streams.kept_for(norms) == {0, 7}
     assert streams.kept_for(B.normtest_grad_norm(lst)) == {0}
+
+
+@pytest.mark.parametrize("on", [0, 7, 9])
+def test_memory_of_lists_that_were_made_on_several_streams(streams, on):
+    """A plan of stream 0, lists of streams 0, 7 and 9: whatever stream a call runs on, the tables and the plan are kept until it has run."""
+    def make(like=None):
+        return B.make_tensor_list([torch.zeros(5), torch.zeros(3)], like=like)
+    grads = make()
+    lists = {0: [grads, make(grads)]}
+    for handle in (7, 9):
+        with streams.on(Stream(handle)):
+            lists[handle] = [make(grads), make(grads)]
+    norms = B.make_norms(grads)
+    for a in (0, 7, 9):
+        for b in (0, 7, 9):
+            x, y, z, u, v = lists[a][0], lists[b][1], lists[b][0], lists[a][1], lists[0][0]
+            for call, used in [(lambda **k: B.normtest_grad_norm(x, norms, **k), (x,)), (lambda **k: B.normtest_clip_grads(x, norms, out=y, **k), (x, y)),
+                               (lambda **k: B.normtest_accumulate(y, x, **k), (x, y)),
+                               (lambda **k: B.normtest_adamw_tensors(x, y, z, u, B.make_hyper(), copy=v, **k), (x, y, z, u, v))]:
+                for own in (False, True):   # the current stream, or one that is named
+                    streams.held.clear()
+                    if own:
+                        call(stream=Stream(on))
+                    else:
+                        with streams.on(Stream(on)):
+                            call()
+                    assert streams.called[-1] == on
+                    for memory in (grads.plan.image, *[lst.table for lst in used]):
+                        assert on in streams.kept_for(memory)
+
+
+def test_the_native_path_is_given_lists_of_their_plans_stream_only(streams, monkeypatch):
+    """It keeps no memory for a stream: it takes a call where the plan and every list were made on the call's stream."""
+    class Fast:
+        def make_list(self, *args):
+            return args
+    monkeypatch.setattr(B, "_fast", Fast())
+    grads = B.make_tensor_list([torch.zeros(5)])
+    alike = B.make_tensor_list([torch.zeros(5)], like=grads)
+    assert grads.native[-1] == alike.native[-1] == 0
+    with streams.on(Stream(7)):
+        assert not B.make_tensor_list([torch.zeros(5)], like=grads).native
+        grads.refresh()
+        assert grads.native[-1] == 0   # its memory is still the first stream's
