@@ -550,7 +550,9 @@ class TensorList:
         host = torch.frombuffer(bytearray(self._records), dtype=torch.uint8) if n else torch.zeros(8, dtype=torch.uint8)
         if self.table is None or self.table.numel() != host.numel():
             self.table = torch.empty(host.numel(), dtype=torch.uint8, device=self.plan.device)
-            self.stream = _stream_handle(None, self.plan.device)   # whose memory it is
+            self.home = torch.cuda.current_stream(self.plan.device)   # whose memory it is
+            self.stream = self.home.cuda_stream
+            self.used = {}   # other streams that calls were made on since: {handle: stream}
         self.table.copy_(host)
         self.addresses = [t.data_ptr() for t in self.tensors]
         self.dtypes = {t.dtype for t in self.tensors}
@@ -560,7 +562,9 @@ class TensorList:
 
     def refresh(self, tensors=None) -> "TensorList":
         """Reads the tensors' addresses again, or those of other tensors of the same shapes and layouts (gradients that were allocated
-        anew).  Ordered on the current stream."""
+        anew).  Calls made before still take the old ones, on whatever stream they run, and calls made after it the new ones: the table is
+        written in place, behind the calls that read it, and the host waits for that.  Replays of a graph that captured a call are not
+        known here: refresh on the stream they are made on, or order them."""
         if tensors is not None:
             tensors = tuple(tensors)
             if len(tensors) != len(self.tensors):
@@ -569,7 +573,12 @@ class TensorList:
             tensors = self.tensors
         self._records = _like_records(tensors, self.plan)
         self.tensors = tensors
+        here = torch.cuda.current_stream(self.plan.device)
+        for handle, stream in {self.stream: self.home, **self.used}.items():
+            if handle != here.cuda_stream:
+                here.wait_stream(stream)
         self._upload()
+        self.used.clear()
         return self
 
     def __len__(self):
@@ -693,6 +702,9 @@ def _list_call(where: str, plan: TensorPlan, lists, norms, stream, fn, *args):
         stream = torch.cuda.current_stream(plan.device) if stream is None else stream
         for memory in others:
             memory.record_stream(stream)
+        for lst in lists:
+            if lst.stream != st:
+                lst.used[st] = stream
 
 
 def _native(lst):

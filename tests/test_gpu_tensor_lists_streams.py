@@ -48,3 +48,18 @@ def test_a_list_made_on_another_stream_and_dropped():
     assert not torch.cuda.current_stream().query() and at not in [t.data_ptr() for t in given]
     torch.cuda.synchronize()
     assert bool((y == 1.0).all())
+
+
+def test_refresh_behind_a_call_on_another_stream():
+    old, new, y = torch.full((50_000,), 2.0, device=DEV), torch.full((50_000,), 3.0, device=DEV), torch.zeros(50_000, device=DEV)
+    src = B.make_tensor_list([old])
+    dst = B.make_tensor_list([y], like=src)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+        B.normtest_accumulate(dst, src)
+    src.refresh([new])
+    B.normtest_accumulate(dst, src)
+    torch.cuda.synchronize()
+    assert bool((y == 5.0).all())

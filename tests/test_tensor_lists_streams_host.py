@@ -121,3 +121,37 @@ def test_the_native_path_is_given_lists_of_their_plans_stream_only(streams, monk
         assert not B.make_tensor_list([torch.zeros(5)], like=grads).native
         grads.refresh()
         assert grads.native[-1] == 0   # its memory is still the first stream's
+
+
+def test_refresh_waits_for_calls_on_other_streams(streams):
+    """The table is written in place (a captured graph reads it there), so it is written behind every call that may still read it."""
+    ran = streams.allocations.ran
+
+    class Waiting(Stream):
+        def wait_stream(self, other):
+            ran.append(("wait", self.cuda_stream, other.cuda_stream))
+
+    def refreshed(lst, on):
+        ran.clear()
+        with streams.on(Waiting(on)):
+            table = lst.table.data_ptr()
+            lst.refresh([torch.ones(5)])
+            assert lst.table.data_ptr() == table
+        at = next(i for i, x in enumerate(ran) if x[0].startswith("aten.copy_"))
+        assert all(x[1] == on for x in ran if x[0] == "wait")
+        assert not [x for x in ran[at:] if x[0] == "wait"]
+        return {x[2] for x in ran if x[0] == "wait"}
+    lst = B.make_tensor_list([torch.zeros(5)])
+    norms = B.make_norms(lst)
+    B.normtest_grad_norm(lst, norms)
+    assert refreshed(lst, 0) == set()             # its own stream: in order
+    assert refreshed(lst, 5) == {0}
+    B.normtest_grad_norm(lst, norms, stream=Stream(7))
+    with streams.on(Stream(9)):
+        B.normtest_clip_grads(lst, norms)
+    assert refreshed(lst, 0) == {7, 9}
+    assert refreshed(lst, 0) == set()             # which it has waited for
+    with streams.on(Stream(7)):
+        other = B.make_tensor_list([torch.zeros(5)], like=lst)
+    B.normtest_accumulate(lst, other)
+    assert refreshed(other, 7) == {0}             # not what the plan's stream does, but what the list was used on
