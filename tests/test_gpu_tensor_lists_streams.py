@@ -40,6 +40,8 @@ def test_a_list_made_on_another_stream_and_dropped():
     with torch.cuda.stream(side):
         dst = B.make_tensor_list([y], like=src)
     at, size = dst.table.data_ptr(), dst.table.numel()
+    B.normtest_accumulate(dst, src, beta=0.0)   # kernels are loaded by their first launch, which takes longer than the wait below
+    torch.cuda.synchronize()
     torch.cuda._sleep(BUSY)
     B.normtest_accumulate(dst, src, beta=0.0, scale=0.5)
     del dst
