@@ -534,7 +534,8 @@ class TensorPlan:
 
 class TensorList:
     """Tensors of one device, as the calls on lists take them: their addresses in a table on the device, and a plan.  The tensors may
-    change their values but not their memory; `refresh` reads their addresses again."""
+    change their values but not their memory, type or shape; `refresh` reads their addresses again.  A list holds its tensors: a gradient
+    that a program drops and makes anew (zero_grad with set_to_none) is another tensor, which the list learns of from refresh only."""
 
     def __init__(self, tensors, plan: TensorPlan, records):
         self.tensors, self.plan = tuple(tensors), plan
@@ -554,11 +555,13 @@ class TensorList:
             self.stream = self.home.cuda_stream
             self.used = {}   # other streams that calls were made on since: {handle: stream}
         self.table.copy_(host)
-        self.addresses = [t.data_ptr() for t in self.tensors]
         self.dtypes = {t.dtype for t in self.tensors}
-        # for the native call path, which takes calls on the stream that table and plan are memory of; None: its calls are left to Python
-        self.native = _fast and self.stream == self.plan.stream and _fast.make_list(
-            self.tensors, self.addresses, ctypes.addressof(self.plan.record), self.plan.record, self.table, self.stream) or None
+        # the list as native code knows it, None: it does not; and for the native call path, which takes calls on the stream that table
+        # and plan are memory of
+        self.held = _fast and _fast.make_list(self.tensors, ctypes.addressof(self.plan.record), self.plan.record, self.table, self.stream) or None
+        self.native = self.held if self.stream == self.plan.stream else None
+        self._made_of = None if self.held else [_place(t) for t in self.tensors]
+        self._held_by = _fast
 
     def refresh(self, tensors=None) -> "TensorList":
         """Reads the tensors' addresses again, or those of other tensors of the same shapes and layouts (gradients that were allocated
@@ -581,8 +584,19 @@ class TensorList:
         self.used.clear()
         return self
 
+    def unchanged(self) -> bool:
+        """Whether the tensors still are what the table on the device says: in a tensor of another type, shape or order at the same
+        address, a call would read and write the old one."""
+        if self.held:
+            return bool(self._held_by.unchanged(self.held))
+        return [_place(t) for t in self.tensors] == self._made_of
+
     def __len__(self):
         return len(self.tensors)
+
+
+def _place(t: torch.Tensor):
+    return t.data_ptr(), t.dtype, t.shape, t.stride()
 
 
 def _check_listed(tensors, device):
@@ -687,8 +701,9 @@ def _list_call(where: str, plan: TensorPlan, lists, norms, stream, fn, *args):
             raise TypeError("%s takes lists made by make_tensor_list, got %s" % (where, type(lst).__name__))
         if lst.plan is not plan:
             raise ValueError("%s: lists of different plans; make one `like` the other" % where)
-        if [t.data_ptr() for t in lst.tensors] != lst.addresses:
-            raise RuntimeError("%s: a tensor of a list has other memory than when the list was made; call its refresh()" % where)
+        if not lst.unchanged():
+            raise RuntimeError("%s: a tensor of a list has other memory, another type or shape than when the list was made; call its refresh()"
+                               % where)
     for x in norms:
         if x is not None and (x.device != plan.device or not x.is_contiguous() or _nbytes(x) < plan.groups * NORM_BYTES):
             raise ValueError("norms must be the contiguous device memory of %d records on %s (make_norms)" % (plan.groups, plan.device))

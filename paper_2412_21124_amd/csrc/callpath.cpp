@@ -259,10 +259,11 @@ PyObject* layer_stats(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- lists of tensors ----
-// A list as the binding made it: its tensors with the addresses that its table on the device holds, and its plan.
+// A list as the binding made it: its tensors, what they were when its table on the device was written, and its plan.
+// Of a tensor: address, type and number of dimensions, sizes, strides; in one array, as every call reads through it (5 lists of 300 tensors: 5 us, 2 more than for addresses alone).
 struct List {
   std::vector<at::Tensor> tensors;
-  std::vector<const void*> addresses;
+  std::vector<int64_t> were;
   const nt_plan* plan;
   const nt_tensor* table;
   c10::Device device = c10::Device(c10::DeviceType::CPU);
@@ -270,6 +271,7 @@ struct List {
   bool all_f32;
   PyObject* owner;   // of the plan's record
 };
+int64_t kind_of(const at::Tensor& t) { return (int64_t)t.scalar_type() << 32 | t.dim(); }
 const char list_name[] = "normtest.list";
 void list_free(PyObject* capsule) {
   List* l = (List*)PyCapsule_GetPointer(capsule, list_name);
@@ -277,40 +279,58 @@ void list_free(PyObject* capsule) {
   Py_XDECREF(l->owner);
   delete l;
 }
-// make_list(tensors, addresses, plan's address, its owner, table, stream's handle); tensors: a tuple, addresses: a list
+// make_list(tensors, plan's address, its owner, table, stream's handle); tensors: a tuple
 PyObject* make_list(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 6, [&]() -> PyObject* {
-    if (!PyTuple_CheckExact(a[0]) || !PyList_CheckExact(a[1]) || PyTuple_GET_SIZE(a[0]) != PyList_GET_SIZE(a[1])) throw Refused();
+  return guarded(n, 5, [&]() -> PyObject* {
+    if (!PyTuple_CheckExact(a[0])) throw Refused();
     std::unique_ptr<List> l(new List());
     l->all_f32 = true;
     for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
       l->tensors.push_back(tensor(PyTuple_GET_ITEM(a[0], i)));
-      l->addresses.push_back(PyLong_AsVoidPtr(PyList_GET_ITEM(a[1], i)));
-      if (!l->addresses.back() && PyErr_Occurred()) throw Refused();
+      const at::Tensor& t = l->tensors.back();
+      l->were.insert(l->were.end(), {(int64_t)(intptr_t)t.data_ptr(), kind_of(t)});
+      l->were.insert(l->were.end(), t.sizes().begin(), t.sizes().end());
+      l->were.insert(l->were.end(), t.strides().begin(), t.strides().end());
       l->all_f32 = l->all_f32 && l->tensors.back().scalar_type() == at::kFloat;
     }
-    l->plan = entry<const nt_plan>(a[2]);
-    const at::Tensor& table = tensor(a[4]);
+    l->plan = entry<const nt_plan>(a[1]);
+    const at::Tensor& table = tensor(a[3]);
     l->table = (const nt_tensor*)table.data_ptr();
     l->device = table.device();
-    l->stream = PyLong_AsVoidPtr(a[5]);
+    l->stream = PyLong_AsVoidPtr(a[4]);
     if (!l->stream && PyErr_Occurred()) throw Refused();
     PyObject* capsule = PyCapsule_New(l.get(), list_name, list_free);
     if (!capsule) throw Refused();
-    Py_INCREF(a[3]);
-    l->owner = a[3];
+    Py_INCREF(a[2]);
+    l->owner = a[2];
     l.release();
     return capsule;
   });
 }
-// The list behind a capsule, its tensors where its table says; `first`: the list whose plan it has to share.
-const List* list_of(PyObject* o, const List* first) {
+const List* held(PyObject* o) {
   if (!PyCapsule_IsValid(o, list_name)) throw Refused();
-  const List* l = (const List*)PyCapsule_GetPointer(o, list_name);
-  if (first && l->plan != first->plan) throw Refused();
-  for (size_t i = 0; i < l->tensors.size(); ++i)
-    if (l->tensors[i].data_ptr() != l->addresses[i]) throw Refused();
+  return (const List*)PyCapsule_GetPointer(o, list_name);
+}
+bool same(const List& l) {
+  const int64_t* was = l.were.data();
+  for (const at::Tensor& t : l.tensors) {
+    if ((int64_t)(intptr_t)t.data_ptr() != was[0] || kind_of(t) != was[1]) return false;
+    was += 2;
+    for (const auto& now : {t.sizes(), t.strides()})
+      for (const int64_t x : now)
+        if (x != *was++) return false;
+  }
+  return true;
+}
+// The list behind a capsule, its tensors what its table says; `first`: the list whose plan it has to share.
+const List* list_of(PyObject* o, const List* first) {
+  const List* l = held(o);
+  if ((first && l->plan != first->plan) || !same(*l)) throw Refused();
   return l;
+}
+// unchanged(list): whether its tensors are what its table says
+PyObject* unchanged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 1, [&] { return PyBool_FromLong(same(*held(a[0]))); });
 }
 const List* list_or_none(PyObject* o, const List* first) { return o == Py_None ? nullptr : list_of(o, first); }
 nt_norm* norms_of(PyObject* o, const List& l, bool required) {
@@ -408,7 +428,7 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init),       FAST(step),        FAST(step_clipped), FAST(step_rows),
-                         FAST(adamw_gbar), FAST(layer_stats), FAST(make_list), FAST(grad_norm), FAST(clip_grads), FAST(accumulate),
+                         FAST(adamw_gbar), FAST(layer_stats), FAST(make_list), FAST(unchanged), FAST(grad_norm), FAST(clip_grads), FAST(accumulate),
                          FAST(adamw_tensors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_callpath", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

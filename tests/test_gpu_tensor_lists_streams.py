@@ -65,3 +65,22 @@ def test_refresh_behind_a_call_on_another_stream():
     B.normtest_accumulate(dst, src)
     torch.cuda.synchronize()
     assert bool((y == 5.0).all())
+
+
+@pytest.mark.parametrize("native", [False, True])
+def test_a_tensor_that_is_another_one_at_the_same_address(monkeypatch, native):
+    """What the table on the device says no longer holds, so no call takes it, until the list is refreshed."""
+    if not native:
+        monkeypatch.setattr(B, "_fast", None)
+    x, y = torch.full((60, 80), 2.0, device=DEV), torch.zeros(60, 80, device=DEV)
+    src = B.make_tensor_list([x])
+    dst = B.make_tensor_list([y], like=src)
+    for new in (y.data[:30], y.data.view(torch.bfloat16), y.data.view(80, 60), y.data.view(-1).as_strided((60, 80), (1, 60))):
+        was, y.data = y.data, new
+        with pytest.raises(RuntimeError, match="refresh"):
+            B.normtest_accumulate(dst, src)
+        y.data = was
+        B.normtest_accumulate(dst, src)
+    y.data = y.data.view(80, 60)
+    B.normtest_accumulate(dst.refresh(), src)
+    assert bool((y == 10.0).all())

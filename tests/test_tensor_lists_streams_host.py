@@ -155,3 +155,36 @@ def test_refresh_waits_for_calls_on_other_streams(streams):
         other = B.make_tensor_list([torch.zeros(5)], like=lst)
     B.normtest_accumulate(lst, other)
     assert refreshed(other, 7) == {0}             # not what the plan's stream does, but what the list was used on
+
+
+def changed_in_place():
+    """What a program may put at a listed tensor's address: (name, function of a (6, 8) tensor)."""
+    def data(new):
+        def change(t):
+            t.data = new(t.data)
+        return change
+    return [("shorter", data(lambda x: x[:3])), ("another type", data(lambda x: x.view(torch.bfloat16))),
+            ("another type of the same size", data(lambda x: x.view(torch.int32))), ("another shape", data(lambda x: x.view(8, 6))),
+            ("other strides", data(lambda x: x.view(-1).as_strided((6, 8), (1, 6)))), ("transposed", lambda t: t.t_()),
+            ("resized", lambda t: t.resize_(2, 8))]
+
+
+@pytest.mark.parametrize("change", [c for _, c in changed_in_place()], ids=[n for n, _ in changed_in_place()])
+@pytest.mark.parametrize("native", [False, True])
+def test_a_tensor_that_is_another_one_at_the_same_address(streams, monkeypatch, change, native):
+    """The table on the device still says what was there: a call would read and write it in the old type and length."""
+    monkeypatch.setattr(B, "_fast", B._load_callpath() if native else None)
+    t = torch.zeros(6, 8)
+    lst = B.make_tensor_list([torch.zeros(5), t])
+    like = B.make_tensor_list([torch.zeros(5), torch.zeros(6, 8)], like=lst)
+    assert bool(lst.held) == native and lst.unchanged()
+    norms = B.make_norms(lst)
+    at = t.data_ptr()
+    change(t)
+    assert t.data_ptr() == at
+    hyper = B.make_hyper()
+    for call in (lambda: B.normtest_grad_norm(lst, norms), lambda: B.normtest_clip_grads(like, norms, out=lst), lambda: B.normtest_accumulate(like, lst),
+                 lambda: B.normtest_accumulate(lst, like), lambda: B.normtest_adamw_tensors(like, like, like, lst, hyper)):
+        with pytest.raises(RuntimeError, match="refresh"):
+            call()
+    assert streams.called == []
