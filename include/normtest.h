@@ -355,7 +355,8 @@ typedef struct {
   double norm;             /* |grad_scale| * norm of the group (0 for a group without elements)                       */
   double coef;             /* min(1, max_norm / (norm + 1e-6)); 1 if max_norm <= 0 or the norm is not finite            */
   float norm32;            /* norm, rounded                                                                            */
-  float factor;            /* grad_scale * coef, rounded: what a gradient is multiplied by                             */
+  float factor;            /* grad_scale * coef, rounded: what a gradient is multiplied by.  Below 2^-126, as where a   */
+                           /* norm is beyond 2^126 max_norm, it has fewer bits, below 2^-150 none: it is zero there    */
   uint32_t status;         /* NT_STATUS_NONFINITE: an element is NaN or infinite; NT_STATUS_ZERO_GRAD_NORM: norm == 0  */
   int32_t clipped;         /* 1 iff coef < 1                                                                           */
   int64_t elements;        /* of the group                                                                             */
@@ -380,12 +381,14 @@ int normtest_list_check(const nt_tensor* list, const nt_tensor* like, int32_t N,
  * NULL if there are none), read by the kernels only; they and their tensors must not change until the call has run.  norms:
  * device or pinned-host arrays of plan->groups records, 8-byte aligned.  Everything is enqueued on the stream, kernel launches only;
  * a graph may capture them.  Returns NT_OK or a negative code; on error nothing was enqueued, except that a failing launch may
- * follow launches that already succeeded.
+ * follow launches that already succeeded.  Scalars (scale, beta, grad_scale, and lr weight_decay and lr / (1 - beta1^k) of hyper) are
+ * rounded to fp32, and NT_ERR_BAD_ARG is returned where that is not finite; a product of a scale and a factor is rounded to fp32 on the device,
+ * where nothing checks it.
  */
 
 /* Norms of the groups of `grads` (any dtypes), and the coefficients for max_norm (<= 0: no clipping, 1).  A group with a NaN or an
  * infinity has the norm NaN or infinity, coefficient 1 and NT_STATUS_NONFINITE: a norm that is not a number clips nothing.
- * grad_scale: finite. */
+ * grad_scale: finite in fp32. */
 int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind, double max_norm, double grad_scale,
                        nt_norm* norms, void* hip_stream);
 

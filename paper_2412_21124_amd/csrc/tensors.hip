@@ -947,8 +947,10 @@ int check_plan(const nt_plan* p) {
 int check_list(const nt_plan& p, const nt_tensor* list) {
   return (p.tensors > 0 && !list) || misaligned8(list) ? NT_ERR_BAD_ARG : NT_OK;
 }
+// the kernels multiply in fp32, where a larger double would be infinite and make NaN of a zero
+bool finite_in_fp32(double x) { return std::isfinite((float)x); }
 int check_norm(int32_t kind, double max_norm, double grad_scale, const nt_norm* norms) {
-  if ((kind != NT_NORM_L2 && kind != NT_NORM_MAX) || std::isnan(max_norm) || !std::isfinite(grad_scale)) return NT_ERR_BAD_ARG;
+  if ((kind != NT_NORM_L2 && kind != NT_NORM_MAX) || std::isnan(max_norm) || !finite_in_fp32(grad_scale)) return NT_ERR_BAD_ARG;
   return !norms || misaligned8(norms) ? NT_ERR_BAD_ARG : NT_OK;
 }
 
@@ -1148,7 +1150,7 @@ int normtest_accumulate(const nt_plan* plan, const nt_tensor* dst, const nt_tens
   if (rc == NT_OK) rc = check_list(*plan, src);
   if (rc == NT_OK && dst_norms) rc = check_norm(kind, max_norm, grad_scale, dst_norms);
   if (rc != NT_OK) return rc;
-  if (!std::isfinite(beta) || !std::isfinite(scale) || misaligned8(src_norms)) return NT_ERR_BAD_ARG;
+  if (!finite_in_fp32(beta) || !finite_in_fp32(scale) || misaligned8(src_norms)) return NT_ERR_BAD_ARG;
   const Layout l = layout_of(*plan);
   const UpdateArgs u = {dst, src, src_norms, scale, (float)beta, 0};
   NormOut o;
@@ -1165,7 +1167,7 @@ int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt
   for (const nt_tensor* list : {grads, w, m, v})
     if (rc == NT_OK) rc = check_list(*plan, list);
   if (rc != NT_OK) return rc;
-  if (!hyper || !std::isfinite(grad_scale) || misaligned8(copy) || misaligned8(norms) || (flags & ~(uint32_t)NT_SKIP_NONFINITE) ||
+  if (!hyper || !finite_in_fp32(grad_scale) || misaligned8(copy) || misaligned8(norms) || (flags & ~(uint32_t)NT_SKIP_NONFINITE) ||
       ((flags & NT_SKIP_NONFINITE) && !norms))
     return NT_ERR_BAD_ARG;
   if (hyper->step < 1 || !(hyper->lr >= 0.0) || !std::isfinite(hyper->lr) || !(hyper->beta1 >= 0.0 && hyper->beta1 < 1.0) ||
@@ -1177,6 +1179,7 @@ int normtest_adamw_tensors(const nt_plan* plan, const nt_tensor* grads, const nt
                        (float)hyper->beta1, (float)(1.0 - hyper->beta1), (float)hyper->beta2, (float)(1.0 - hyper->beta2),
                        (float)(1.0 - hyper->lr * hyper->weight_decay), (float)(hyper->lr / bc1), (float)(1.0 / std::sqrt(bc2)),
                        (float)hyper->eps};
+  if (!std::isfinite(u.decay) || !std::isfinite(u.step_size)) return NT_ERR_BAD_ARG;
   const Layout l = layout_of(*plan);
   const Cut cut = cut_of(*plan, l, 0);
   ListArgs a = {(const Shape*)((char*)plan->image + l.shapes), cut.items, 0};

@@ -243,3 +243,20 @@ def test_lists_refuse_what_is_not_on_the_device():
                  lambda: B.normtest_adamw_tensors([], [], [], [], B.make_hyper())):
         with pytest.raises(TypeError, match="make_tensor_list"):
             call()
+
+
+def test_scalars_that_fp32_does_not_hold_are_refused():
+    """The kernels multiply in fp32: a finite double past its range would be infinite there, and make NaN of a zero."""
+    L = B.lib()
+    plan, _ = plan_of([(1, 5)])
+    plan.image = 0x10000
+    ok, bad = ctypes.byref(plan), B.NT_ERR_BAD_ARG
+    for x in (1e39, -1e39, 1e300):
+        assert L.normtest_grad_norm(ok, 0x1000, 0, 1.0, x, 0x2000, None) == bad
+        assert L.normtest_accumulate(ok, 0x1000, 0x3000, x, 1.0, None, 0, 1.0, 1.0, None, None) == bad
+        assert L.normtest_accumulate(ok, 0x1000, 0x3000, 1.0, x, None, 0, 1.0, 1.0, None, None) == bad
+        assert L.normtest_accumulate(ok, 0x1000, 0x3000, 1.0, 1.0, None, 0, 1.0, x, 0x2000, None) == bad
+        assert L.normtest_adamw_tensors(ok, 0x1000, 0x1000, 0x1000, 0x1000, None, ctypes.byref(B.make_hyper()), x, None, 0, None) == bad
+    for wrong in [dict(lr=1e39), dict(lr=1e38, beta1=0.99), dict(lr=1e20, weight_decay=1e20)]:
+        hyper = ctypes.byref(B.make_hyper(**wrong))
+        assert L.normtest_adamw_tensors(ok, 0x1000, 0x1000, 0x1000, 0x1000, None, hyper, 1.0, None, 0, None) == bad, wrong
