@@ -68,6 +68,7 @@ enum {
   NT_ERR_UNSUPPORTED = -2,
   NT_ERR_WORKSPACE_TOO_SMALL = -3,
   NT_ERR_TOO_LARGE = -4,
+  NT_ERR_SHARED_MEMORY = -5,   /* two tensors of a list have an element in common */
   NT_ERR_HIP_BASE = -1000
 };
 
@@ -372,8 +373,9 @@ enum { NT_SKIP_NONFINITE = 1u };   /* leave the tensors of a group alone whose s
 int normtest_plan_make(const nt_tensor* tensors, int32_t N, int32_t G, nt_plan* plan, void* image, size_t image_bytes);
 
 /* Host check of a list before it is copied to the device: the shapes are those of `like` (host arrays of N), addresses are there
- * and element-aligned, ld >= cols where rows > 1, and every dtype's bit (1 << dtype) is in `dtypes`.  NT_OK, NT_ERR_BAD_ARG or,
- * for a dtype, NT_ERR_UNSUPPORTED. */
+ * and element-aligned, ld >= cols where rows > 1, every dtype's bit (1 << dtype) is in `dtypes`, and no two tensors share memory (slices
+ * of one matrix may lie between each other's rows).  NT_OK, NT_ERR_BAD_ARG, for a dtype NT_ERR_UNSUPPORTED, for shared memory
+ * NT_ERR_SHARED_MEMORY; NT_ERR_TOO_LARGE if there is no host memory to look for that in. */
 int normtest_list_check(const nt_tensor* list, const nt_tensor* like, int32_t N, uint32_t dtypes);
 
 /*

@@ -29,6 +29,7 @@ NT_STATUS_T_SATURATED = 16
 NT_STATUS_NO_STATS = 32
 NT_STATUS_BAD_RANGE = 64
 NT_OK, NT_ERR_BAD_ARG, NT_ERR_UNSUPPORTED, NT_ERR_WORKSPACE_TOO_SMALL, NT_ERR_TOO_LARGE, NT_ERR_HIP_BASE = 0, -1, -2, -3, -4, -1000
+NT_ERR_SHARED_MEMORY = -5
 
 
 class nt_hyper(ctypes.Structure):
@@ -538,16 +539,21 @@ class TensorList:
     that a program drops and makes anew (zero_grad with set_to_none) is another tensor, which the list learns of from refresh only."""
 
     def __init__(self, tensors, plan: TensorPlan, records):
-        self.tensors, self.plan = tuple(tensors), plan
-        self._records = records
+        self.plan = plan
         self.table = None
+        self._check(records)
+        self.tensors, self._records = tuple(tensors), records
         self._upload()
+
+    def _check(self, records):
+        rc = lib().normtest_list_check(records, self.plan.records, len(records), ANY_DTYPE)
+        if rc == NT_ERR_SHARED_MEMORY:
+            raise ValueError("two tensors of the list share memory (a tied weight is listed once)")
+        if rc != NT_OK:
+            raise NormtestError(rc, "normtest_list_check")
 
     def _upload(self):
         n = len(self.tensors)
-        rc = lib().normtest_list_check(self._records, self.plan.records, n, ANY_DTYPE)
-        if rc != NT_OK:
-            raise NormtestError(rc, "normtest_list_check")
         host = torch.frombuffer(bytearray(self._records), dtype=torch.uint8) if n else torch.zeros(8, dtype=torch.uint8)
         if self.table is None or self.table.numel() != host.numel():
             self.table = torch.empty(host.numel(), dtype=torch.uint8, device=self.plan.device)
@@ -574,8 +580,9 @@ class TensorList:
                 raise ValueError("the list has %d tensors, got %d" % (len(self.tensors), len(tensors)))
         else:
             tensors = self.tensors
-        self._records = _like_records(tensors, self.plan)
-        self.tensors = tensors
+        records = _like_records(tensors, self.plan)
+        self._check(records)
+        self.tensors, self._records = tensors, records
         here = torch.cuda.current_stream(self.plan.device)
         for handle, stream in {self.stream: self.home, **self.used}.items():
             if handle != here.cuda_stream:
@@ -633,7 +640,7 @@ def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, lik
     groups: a number from 0 on for every tensor, whose norms are then taken group by group (default: one group); num_groups: how many there
     are, where the last may have no tensor (default: up to the largest number).
     like: a list of corresponding tensors (same sizes; contiguous, or with the same dimensions in the same order in memory), whose plan and
-    groups are shared: gradients, weights and moments of one model.  Tensors are dense, or rows of one stride (column slices); a plan
+    groups are shared: gradients, weights and moments of one model.  No two tensors share memory.  Tensors are dense, or rows of one stride (column slices); a plan
     made from dense tensors does not serve sliced ones.  device: of an empty sequence.
     Making a list copies its tables to the device and waits for that; make it once and keep it."""
     tensors = tuple(tensors)

@@ -2798,6 +2798,7 @@ const char* normtest_strerror(int code) {
     case NT_ERR_BAD_ARG: return "bad argument (null or misaligned pointer, J < 2, d < 0, ld < d, or invalid hyper-parameters)";
     case NT_ERR_UNSUPPORTED: return "unsupported gradient dtype";
     case NT_ERR_WORKSPACE_TOO_SMALL: return "workspace smaller than normtest_workspace_bytes(J, d)";
+    case NT_ERR_SHARED_MEMORY: return "two tensors of a list share memory";
     case NT_ERR_TOO_LARGE: return "d beyond normtest_static_max_coords(J): the built-in scratch cannot hold the partial sums";
     default: break;
   }

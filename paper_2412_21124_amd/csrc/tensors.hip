@@ -15,10 +15,12 @@
 // alone fixes.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <initializer_list>
+#include <memory>
 #include <new>
 
 #include "normtest.h"
@@ -940,6 +942,40 @@ Cut cut_of(const nt_plan& p, const Layout& l, int k) {
           (double*)(b + l.sums[k]), p.items[k], p.slabs[k], NT_LONG_BLOCKS, run_of(p, k), slab_shift(p.slots[k])};
 }
 
+// Where a tensor's elements lie, in bytes: rows of `width`, `stride` apart (dense tensors: one row).
+struct Span {
+  uint64_t begin, end, rows, width, stride;
+};
+// whether b's row from `at` on, `width` bytes, has bytes of a; at >= a.begin
+bool meets(const Span& a, uint64_t at, uint64_t width) {
+  const uint64_t row = (at - a.begin) / a.stride, in = (at - a.begin) % a.stride;
+  return row < a.rows && (in < a.width || (row + 1 < a.rows && a.stride - in < width));
+}
+// a.begin <= b.begin < a.end
+bool share(const Span& a, const Span& b) {
+  if (a.rows == 1) return true;
+  // rows that are as far apart as a's lie in each of a's as b's first does; others are looked at one by one, as far as a reaches
+  const uint64_t looked_at = a.stride == b.stride ? 1 : b.rows;
+  for (uint64_t r = 0; r < looked_at && b.begin + r * b.stride < a.end; ++r)
+    if (meets(a, b.begin + r * b.stride, b.width)) return true;
+  return false;
+}
+// whether two of n spans, in ascending order of begin, share memory; open: room for n
+bool any_share(const Span* spans, int32_t n, int32_t* open) {
+  int32_t nopen = 0;   // those that reach to the present one or beyond it
+  for (int32_t i = 0; i < n; ++i) {
+    int32_t kept = 0;
+    for (int32_t j = 0; j < nopen; ++j)
+      if (spans[open[j]].end > spans[i].begin) {
+        if (share(spans[open[j]], spans[i])) return true;
+        open[kept++] = open[j];
+      }
+    open[kept++] = i;
+    nopen = kept;
+  }
+  return false;
+}
+
 int check_plan(const nt_plan* p) {
   if (!p || p->magic != NT_PLAN_MAGIC || !p->image || ((uintptr_t)p->image & 15u) || p->groups < 1 || p->tensors < 0) return NT_ERR_BAD_ARG;
   return NT_OK;
@@ -1108,7 +1144,29 @@ int normtest_list_check(const nt_tensor* list, const nt_tensor* like, int32_t N,
     if (t.rows == 0 || t.cols == 0) continue;
     if (!t.data || ((uintptr_t)t.data & ((1u << size_shift(t.dtype)) - 1)) || (t.rows > 1 && t.ld < t.cols)) return NT_ERR_BAD_ARG;
   }
-  return NT_OK;
+  if (N < 2) return NT_OK;
+  const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[N]);
+  const std::unique_ptr<int32_t[]> open(new (std::nothrow) int32_t[N]);
+  if (!spans || !open) return NT_ERR_TOO_LARGE;
+  int32_t n = 0;
+  for (int32_t i = 0; i < N; ++i) {
+    const nt_tensor& t = list[i];
+    if (t.rows == 0 || t.cols == 0) continue;
+    Span s = {(uintptr_t)t.data, 0, (uint64_t)t.rows, (uint64_t)t.cols, (uint64_t)(t.rows > 1 ? t.ld : t.cols)};
+    if (s.width == s.stride) {
+      if (__builtin_mul_overflow(s.rows, s.width, &s.width)) return NT_ERR_BAD_ARG;
+      s.rows = 1;
+      s.stride = s.width;
+    }
+    uint64_t size = 0;   // from the first element to the last
+    if (__builtin_mul_overflow(s.width, 1ull << size_shift(t.dtype), &s.width) || __builtin_mul_overflow(s.stride, 1ull << size_shift(t.dtype), &s.stride) ||
+        __builtin_mul_overflow(s.rows - 1, s.stride, &size) || __builtin_add_overflow(size, s.width, &size) ||
+        __builtin_add_overflow(s.begin, size, &s.end))
+      return NT_ERR_BAD_ARG;
+    spans[n++] = s;
+  }
+  std::sort(spans.get(), spans.get() + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  return any_share(spans.get(), n, open.get()) ? NT_ERR_SHARED_MEMORY : NT_OK;
 }
 
 int normtest_grad_norm(const nt_plan* plan, const nt_tensor* grads, int32_t kind, double max_norm, double grad_scale, nt_norm* norms,

@@ -260,3 +260,29 @@ def test_scalars_that_fp32_does_not_hold_are_refused():
     for wrong in [dict(lr=1e39), dict(lr=1e38, beta1=0.99), dict(lr=1e20, weight_decay=1e20)]:
         hyper = ctypes.byref(B.make_hyper(**wrong))
         assert L.normtest_adamw_tensors(ok, 0x1000, 0x1000, 0x1000, 0x1000, None, hyper, 1.0, None, 0, None) == bad, wrong
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_the_check_finds_shared_elements(seed):
+    """Against the sets of bytes: few tensors of any rows, strides and types in little memory, so that about half of the lists share some."""
+    rng = random.Random(seed)
+    found = [0, 0]
+    for _ in range(400):
+        tensors, held, shared = [], set(), False
+        for _ in range(rng.choice([2, 2, 3, 5])):
+            dtype = rng.choice([B.NT_F32, B.NT_BF16, B.NT_F16])
+            size = 4 if dtype == B.NT_F32 else 2
+            rows, cols = rng.choice([(1, rng.randrange(40)), (rng.randrange(1, 12), rng.randrange(0, 9))])
+            ld = cols + rng.choice([0, 1, 7, rng.randrange(40), 30 - cols])
+            at = 0x1000 + size * rng.randrange(600)
+            tensors.append(B.nt_tensor(at, rows, cols, ld, dtype, 0))
+            mine = {at + size * (r * ld + c) + b for r in range(rows) for c in range(cols) for b in range(size)}
+            shared |= bool(mine & held)
+            held |= mine
+        records = (B.nt_tensor * len(tensors))(*tensors)
+        rc = B.lib().normtest_list_check(records, records, len(tensors), B.ANY_DTYPE)
+        assert rc == (B.NT_ERR_SHARED_MEMORY if shared else B.NT_OK)
+        found[shared] += 1
+    assert min(found) > 50
+    far = (B.nt_tensor * 2)(B.nt_tensor(0x1000, 2, 5, 1 << 62, 0, 0), B.nt_tensor(0x2000, 1, 5, 5, 0, 0))
+    assert B.lib().normtest_list_check(far, far, 2, B.ANY_DTYPE) == B.NT_ERR_BAD_ARG

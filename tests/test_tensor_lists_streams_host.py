@@ -188,3 +188,26 @@ def test_a_tensor_that_is_another_one_at_the_same_address(streams, monkeypatch, 
         with pytest.raises(RuntimeError, match="refresh"):
             call()
     assert streams.called == []
+
+
+def test_no_two_tensors_of_a_list_share_elements(streams):
+    """A tied weight that is listed twice would be updated by two blocks at once."""
+    flat, wide = torch.zeros(1000), torch.zeros(20, 50)
+    a, b = flat[:300], flat[300:]
+    apart = [[a, b], [b, a], [a, torch.zeros(0), torch.zeros(0), b], [flat[:0], flat, flat[1000:]], [wide[:, :20], wide[:, 20:]],
+             [wide[:, 30:], wide[:, :30], wide[:0]], [wide[:10], wide[10:]], [wide[:10, :20], wide[10:, :20], wide[:, 20:]], [wide[::2], wide[1::2]],
+             [wide[:10, 40:], wide[10:, :5]], [wide[:, 3:4], wide[:, 4:5]], [wide.view(-1)[::2], wide.view(-1)[1::2]]]
+    shared = [[a, a], [flat, a], [a, torch.zeros(3), flat[299:301]], [flat, flat.view(10, 100)], [flat, flat.view(torch.bfloat16)[1999:]],
+              [wide[:, :20], wide[:, 19:]], [wide, wide[3:4, 7:8]], [wide[:, :20], wide.view(-1)[949:952]], [wide[5:, :30], wide[:6, 29:31]],
+              [wide[:, 3:4], wide[:, 3:4]], [wide.view(-1)[::2], wide.view(-1)[::2]], [wide[:, :20].t(), wide[0, 19:30]]]
+    for tensors in apart:
+        B.make_tensor_list(tensors).refresh(tensors[::1])
+    for tensors in shared:
+        with pytest.raises(ValueError, match="share memory"):
+            B.make_tensor_list(tensors)
+        lst = B.make_tensor_list([t.clone(memory_format=torch.contiguous_format) for t in tensors])
+        if all(t.is_contiguous() for t in tensors):
+            with pytest.raises(ValueError, match="share memory"):
+                B.make_tensor_list(tensors, like=lst)
+            with pytest.raises(ValueError, match="share memory"):
+                lst.refresh(tensors)
