@@ -606,10 +606,14 @@ def _place(t: torch.Tensor):
     return t.data_ptr(), t.dtype, t.shape, t.stride()
 
 
+def _check_tensor(t):
+    if not isinstance(t, torch.Tensor) or t.layout != torch.strided:
+        raise TypeError("a list holds dense torch tensors, got %s" % (t.layout if isinstance(t, torch.Tensor) else type(t).__name__))
+
+
 def _check_listed(tensors, device):
     for t in tensors:
-        if not isinstance(t, torch.Tensor) or t.layout != torch.strided:
-            raise TypeError("a list holds dense torch tensors")
+        _check_tensor(t)
         if t.dtype not in _LIST_DTYPES:
             raise TypeError("tensors of a list must be float32, bfloat16 or float16, got %s" % t.dtype)
         if t.device != device:
@@ -652,6 +656,8 @@ def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, lik
         return TensorList(tensors, like.plan, _like_records(tensors, like.plan))
     if not tensors and device is None:
         raise ValueError("an empty list needs a device")
+    if tensors:
+        _check_tensor(tensors[0])
     device = tensors[0].device if tensors else torch.device(device)
     if device.type == "cuda" and device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())

@@ -286,3 +286,10 @@ def test_the_check_finds_shared_elements(seed):
     assert min(found) > 50
     far = (B.nt_tensor * 2)(B.nt_tensor(0x1000, 2, 5, 1 << 62, 0, 0), B.nt_tensor(0x2000, 1, 5, 5, 0, 0))
     assert B.lib().normtest_list_check(far, far, 2, B.ANY_DTYPE) == B.NT_ERR_BAD_ARG
+
+
+def test_a_list_of_something_else_than_tensors():
+    """The first entry like any other: a gradient that backward() has not made is None."""
+    for bad in ([None], [None, torch.zeros(3)], [3.0], [torch.zeros(3).numpy()]):
+        with pytest.raises(TypeError, match="torch tensors"):
+            B.make_tensor_list(bad)
