@@ -106,3 +106,11 @@ def test_adamw(launches):
     assert got[3] == [("k_adamw", "", [2, 1024], 16384, 1024, 82000)] * 3
     assert got[4] == [("k_adamw", "", [1, 512], 16384, 512, 0)]      # mostly rows: not kept in step
     assert got[5] == [("k_adamw", "", [2, 512], 32768, 512, 0)]
+
+
+def test_norms_of_very_many_groups(launches):
+    """A launch has at most 2^20 blocks, as a grid ends at 2^32 threads: the blocks of the norm go on in another one."""
+    got = launches([_call("norm", [(1, 5, 2)], G=(1 << 20) + 3), _call("norm", [(1, 1 << 21, 1)], G=(1 << 22) + 1)])
+    assert got[0] == [("k_norm", "l2", [0], 1 << 20, 256, 0), ("k_norm", "l2", [0], 3, 256, 0)]
+    items = (1 << 21) // 8192 + (1 << 22)                            # those of one group, one for every other: in runs of two
+    assert got[1] == [("k_norm", "l2", [0], 1 << 20, 256, 0)] * 2 + [("k_norm", "l2", [0], items // 2 - (1 << 21), 256, 0)]
