@@ -668,6 +668,8 @@ def make_tensor_list(tensors, groups=None, num_groups: Optional[int] = None, lik
     num_groups = max(groups, default=0) + 1 if num_groups is None else int(num_groups)
     if num_groups <= max(groups, default=0):
         raise ValueError("num_groups is %d, but a tensor is in group %d" % (num_groups, max(groups, default=0)))
+    if num_groups >= 1 << 31:
+        raise ValueError("a list has fewer than 2^31 groups, got %d" % num_groups)
     made, layouts = [], []
     for t, g in zip(tensors, groups):
         rows, cols, ld, order = _rows_of(t)

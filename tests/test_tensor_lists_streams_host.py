@@ -211,3 +211,10 @@ def test_no_two_tensors_of_a_list_share_elements(streams):
                 B.make_tensor_list(tensors, like=lst)
             with pytest.raises(ValueError, match="share memory"):
                 lst.refresh(tensors)
+
+
+def test_group_numbers_past_32_bits(streams):
+    """They would be another group's in the library's records."""
+    for kw in (dict(groups=[1 << 32]), dict(num_groups=(1 << 32) + 1), dict(groups=[(1 << 31) - 1])):
+        with pytest.raises(ValueError, match="2\\^31"):
+            B.make_tensor_list([torch.zeros(3)], **kw)
