@@ -31,8 +31,7 @@ def build_library(out: str = LIB, quiet: bool = True) -> str:
         objects.append("%s.%s.o" % (tmp, os.path.splitext(os.path.basename(src))[0]))
         running.append(_start(["hipcc", *HIPCC_FLAGS, "-I", INCLUDE, "-c", "-o", objects[-1], src]))
     try:
-        said = [_finish(r) for r in running]
-        said.append(_finish(_start(["hipcc", *HIPCC_FLAGS, "-shared", "-o", tmp, *objects])))
+        said = _finish(running) + _finish([_start(["hipcc", *HIPCC_FLAGS, "-shared", "-o", tmp, *objects])])
     finally:
         for o in objects:
             if os.path.exists(o):
@@ -48,11 +47,12 @@ def _start(cmd):
     return cmd, subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
 
 
-def _finish(started) -> str:
-    cmd, process = started
-    _, said = process.communicate()
-    if process.returncode != 0:
-        raise RuntimeError("hipcc failed:\n%s\n%s" % (" ".join(cmd), said))
+def _finish(running) -> list:
+    """What each of them printed, once all have ended."""
+    said = [process.communicate()[1] for _, process in running]
+    for (cmd, process), text in zip(running, said):
+        if process.returncode != 0:
+            raise RuntimeError("hipcc failed:\n%s\n%s" % (" ".join(cmd), text))
     return said
 
 
