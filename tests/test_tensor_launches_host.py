@@ -114,3 +114,10 @@ def test_norms_of_very_many_groups(launches):
     assert got[0] == [("k_norm", "l2", [0], 1 << 20, 256, 0), ("k_norm", "l2", [0], 3, 256, 0)]
     items = (1 << 21) // 8192 + (1 << 22)                            # those of one group, one for every other: in runs of two
     assert got[1] == [("k_norm", "l2", [0], 1 << 20, 256, 0)] * 2 + [("k_norm", "l2", [0], items // 2 - (1 << 21), 256, 0)]
+
+
+def test_adamw_of_dense_tensors_and_rows(launches):
+    """Fewer than half of the elements in rows: kept in step, also the rows' items."""
+    got = launches([_call("adamw", [(1, 45_000_001), (3001, 5003), (2000, 1001), (1, 7)])])
+    items = 10_987 + 2 * 3001 + 500 + 1
+    assert got[0] == [("k_adamw", "", [1, 1024], n, 1024, 82000) for n in (16_384, items - 16_384)]
