@@ -15,9 +15,10 @@ DEV = "cuda:0"
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
-def test_norms_of_more_groups_than_a_launch_has_blocks():
-    """Groups without elements beside the first, the last and those at the seam between two launches."""
-    ids = [0, (1 << 20) - 1, 1 << 20, (1 << 20) + 2]
+@pytest.mark.parametrize("G", [(1 << 20) + 3, (1 << 21) + 5])
+def test_norms_of_very_many_groups(G):
+    """Groups without elements beside those of four tensors, in runs of two and three items."""
+    ids = [0, (1 << 20) - 1, 1 << 20, G - 1]
     x = [torch.full((n,), 2.0, device=DEV) for n in (5, 9000, 4097, 3)]
     lst = B.make_tensor_list(x, groups=ids)
     views = B.norm_views(B.normtest_grad_norm(lst, max_norm=1.0))

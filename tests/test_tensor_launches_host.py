@@ -109,11 +109,12 @@ def test_adamw(launches):
 
 
 def test_norms_of_very_many_groups(launches):
-    """A launch has at most 2^20 blocks, as a grid ends at 2^32 threads: the blocks of the norm go on in another one."""
-    got = launches([_call("norm", [(1, 5, 2)], G=(1 << 20) + 3), _call("norm", [(1, 1 << 21, 1)], G=(1 << 22) + 1)])
-    assert got[0] == [("k_norm", "l2", [0], 1 << 20, 256, 0), ("k_norm", "l2", [0], 3, 256, 0)]
-    items = (1 << 21) // 8192 + (1 << 22)                            # those of one group, one for every other: in runs of two
-    assert got[1] == [("k_norm", "l2", [0], 1 << 20, 256, 0)] * 2 + [("k_norm", "l2", [0], items // 2 - (1 << 21), 256, 0)]
+    """A grid ends at 2^32 threads, so the norm's blocks take as many items as make one launch of 2^20 of them."""
+    got = launches([_call("norm", [(1, 5, 2)], G=1 << 20), _call("norm", [(1, 5, 2)], G=(1 << 20) + 3), _call("norm", [(1, 5, 2)], G=(1 << 24) + 1),
+                    _call("norm", [(1, 1 << 21, 1)], G=(1 << 22) + 1), _call("norm", [(1 << 12, 1 << 10, 1)], G=(1 << 21) + 1)])
+    items = [1 << 20, (1 << 20) + 3, (1 << 24) + 1, (1 << 21) // 8192 + (1 << 22), (1 << 12) // 8 + (1 << 21)]
+    for g, n, run in zip(got, items, [1, 2, 17, 5, 3]):
+        assert g == [("k_norm", "l2", [0], -(-n // run), 256, 0)] and -(-n // run) <= 1 << 20
 
 
 def test_adamw_of_dense_tensors_and_rows(launches):
