@@ -68,7 +68,7 @@ enum {
   NT_ERR_UNSUPPORTED = -2,
   NT_ERR_WORKSPACE_TOO_SMALL = -3,
   NT_ERR_TOO_LARGE = -4,
-  NT_ERR_SHARED_MEMORY = -5,   /* two tensors of a list have an element in common */
+  NT_ERR_SHARED_MEMORY = -6,   /* two tensors of a list have an element in common */
   NT_ERR_HIP_BASE = -1000
 };
 

@@ -29,7 +29,7 @@ NT_STATUS_T_SATURATED = 16
 NT_STATUS_NO_STATS = 32
 NT_STATUS_BAD_RANGE = 64
 NT_OK, NT_ERR_BAD_ARG, NT_ERR_UNSUPPORTED, NT_ERR_WORKSPACE_TOO_SMALL, NT_ERR_TOO_LARGE, NT_ERR_HIP_BASE = 0, -1, -2, -3, -4, -1000
-NT_ERR_SHARED_MEMORY = -5
+NT_ERR_SHARED_MEMORY = -6
 
 
 class nt_hyper(ctypes.Structure):
