@@ -311,7 +311,8 @@ uint32_t normtest_schedule_flags(int64_t step, int64_t test_interval, int64_t b_
 
 /* ------------------------------------------------------------------------------------------------------------------
  * Lists of tensors.  A model's gradients, weights and moments are many tensors, not one vector.  The calls below take
- * lists of them, each in one launch or two whatever the number of tensors:
+ * lists of them.  How many kernels a call launches depends on the elements, not on the tensors: one, where tensors are written one per 2^20
+ * pieces of up to 4096 elements, and from 5 2^23 elements on, mostly in dense tensors, AdamW one per 2^14 pieces (2^26 elements):
  *
  *     normtest_grad_norm       N_g = |s| sqrt(sum of x^2), or |s| max |x|, over the tensors of group g,
  *                              c_g = min(1, max_norm / (N_g + 1e-6)) and the factor f_g = s c_g

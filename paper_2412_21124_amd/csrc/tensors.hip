@@ -1,12 +1,12 @@
 // Norms, clipping, accumulation and AdamW over lists of tensors, hand-written for gfx950 (MI355X).
 //
 // A list is cut into items, pieces of one tensor each, by a plan that the host makes once (normtest_plan_make): for the calls that
-// write, items of NT_ITEM elements, four for each thread of a block; for the norm alone, which only reads, longer ones.  A block
-// takes one item: which tensor it belongs to and where it begins is one 16-byte record, the tensor's address a second one.
+// write, items of NT_ITEM elements, one for each block, 4 to 16 elements a thread; for the norm alone, which only reads, longer ones, of
+// which a block takes several.  Which tensor an item belongs to and where it begins is one 16-byte record, the tensor's address a second one.
 // All of it is bound by memory (2 operations a byte), so nothing here is a matrix product; short lists are bound by the way from a launch
 // over the two records to the elements and back (some 4 us), and a norm by the counting and adding up behind it (1 to 2 us more).  Measured:
-// norm of 1.5e9 bf16 432 us, 6.9 TB/s (a plain read of the same bytes 400); accumulation of 304.6M bf16 291 us, 6.3 TB/s; norm and clipped
-// AdamW of 1.1e9 bf16 with a bf16 copy 5.6 ms, 5.9 TB/s with the gradients read twice (an arithmetic-free mix of the kind 5.6 to 5.9).
+// norm of 1.5e9 bf16 433 us, 6.9 TB/s (a plain read of the same bytes 400); accumulation of 304.6M bf16 296 us, 6.2 TB/s; norm and clipped
+// AdamW of 1.1e9 bf16 with a bf16 copy 5.7 ms, 5.8 TB/s with the gradients read twice (an arithmetic-free mix of the kind 5.6 to 5.9).
 //
 // Norms.  x^2 is formed and summed in fp64, so no finite value overflows and no rounding of the sum is seen; the largest
 // magnitude is the largest |x| by its bits as an integer, where a NaN is larger than infinity and so survives.  A block leaves
