@@ -222,7 +222,7 @@ def prepare(case, seed):
         if op == "matmul":
             s["a_mx"] = B.MxTensor(*s["a"], case["inner"], forms[case["form"]])
             s["b_mx"] = B.MxTensor(*s["b"], case["inner"], forms[case["form_b"]])
-            need = B.normtest_mx_matmul_workspace_bytes(s["a_mx"], s["b_mx"])
+            need = B.normtest_mx_matmul_workspace_bytes(s["a_mx"], s["b_mx"], s["out"].dtype)
             s["workspace"] = torch.empty(need, dtype=torch.uint8, device=DEVICE)
         if op == "norm":
             s["sum"], s["rstd"] = like(), torch.empty(rows, device=DEVICE)
