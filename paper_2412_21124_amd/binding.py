@@ -20,6 +20,8 @@ from . import build as _build
 NT_F32, NT_BF16, NT_F16 = 0, 1, 2
 NT_NORM_L2, NT_NORM_MAX = 0, 1
 NT_SKIP_NONFINITE = 1
+NT_MX_E2M1, NT_MX_E4M3 = 0, 1
+NT_MX_FIT = 1
 NT_DO_STATS, NT_DO_ADAMW, NT_PARTIAL, NT_WRITE_GBAR, NT_COORD_TEST, NT_ONE_PASS = 1, 2, 4, 8, 16, 32
 NT_STATUS_NONFINITE = 1
 NT_STATUS_ZERO_GRAD_NORM = 2
@@ -106,6 +108,11 @@ class nt_norm(ctypes.Structure):
 NORM_BYTES = ctypes.sizeof(nt_norm)
 
 
+class nt_mx(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("scale_ld", ctypes.c_int64), ("format", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class NormtestError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -187,6 +194,18 @@ def lib(path: Optional[str] = None):
         L.normtest_adamw_tensors.argtypes = [plan, vp, vp, vp, vp, vp, ctypes.POINTER(nt_hyper), dbl, vp, ctypes.c_uint32, vp]
         for name in ("plan_make", "list_check", "grad_norm", "clip_grads", "accumulate", "adamw_tensors"):
             getattr(L, "normtest_" + name).restype = ctypes.c_int
+        mx, size, c_int, u32 = ctypes.POINTER(nt_mx), ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32
+        L.normtest_mx_quantize.argtypes = [vp, c_int, i64, i64, i64, vp, i64, mx, mx, u32, vp]
+        L.normtest_mx_dequantize.argtypes = [mx, vp, c_int, i64, vp]
+        L.normtest_mx_matmul.argtypes = [mx, mx, dbl, dbl, vp, c_int, i64, vp, size, vp]
+        L.normtest_mx_matmul_workspace_bytes.argtypes = [i64, i64, i64, c_int, c_int, c_int]
+        L.normtest_rms_norm.argtypes = [vp, i64, vp, i64, vp, dbl, c_int, i64, i64, vp, i64, vp, i64, mx, vp, u32, vp]
+        L.normtest_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, c_int, i64, i64, vp, i64, vp, dbl, dbl, vp, size, vp]
+        L.normtest_rms_norm_workspace_bytes.argtypes = [i64, i64]
+        for name in ("mx_quantize", "mx_dequantize", "mx_matmul", "rms_norm", "rms_norm_backward"):
+            getattr(L, "normtest_" + name).restype = c_int
+        for name in ("mx_matmul", "rms_norm"):
+            getattr(L, "normtest_%s_workspace_bytes" % name).restype = size
         L.normtest_calib_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
         L.normtest_calib_copy.restype = ctypes.c_int
         L.normtest_calib_streams.argtypes = [vp, ctypes.c_size_t, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -820,6 +839,231 @@ def normtest_adamw_tensors(grads: TensorList, w: TensorList, m: TensorList, v: T
     tables = [lst.table.data_ptr() if isinstance(lst, TensorList) else None for lst in lists]
     _list_call(where, plan, lists, (norms,), stream, lib().normtest_adamw_tensors, *tables[:4], tables[4] if copy is not None else None,
                ctypes.byref(hyper), float(grad_scale), _ptr(norms), NT_SKIP_NONFINITE if skip_nonfinite else 0)
+
+
+# ---- microscaled matrices --------------------------------------------------------------------
+
+_MX_BLOCK = 32
+_MX_BLOCK_BYTES = {NT_MX_E2M1: 16, NT_MX_E4M3: 32}
+
+
+class MxTensor:
+    """A microscaled matrix: rows x cols elements in 4 bits (NT_MX_E2M1) or 8 (NT_MX_E4M3), 32 of a row to a scale.
+
+    codes, scales: uint8 device tensors with a row for every row, of at least ceil(cols / 32) blocks' codes (16 or 32 bytes each; rows begin at
+    multiples of 16 bytes) and that many scales.  Elements behind column cols in a row's last block are zero codes.  make_mx allocates one."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, format: int = NT_MX_E2M1):
+        if format not in _MX_BLOCK_BYTES:
+            raise ValueError("format must be NT_MX_E2M1 or NT_MX_E4M3, got %r" % (format,))
+        blocks = (cols + _MX_BLOCK - 1) // _MX_BLOCK
+        if cols < 0:
+            raise ValueError("cols must not be negative, got %d" % cols)
+        for name, t, least in (("codes", codes, blocks * _MX_BLOCK_BYTES[format]), ("scales", scales, blocks)):
+            if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError("%s must be a 2-D uint8 tensor with a contiguous last axis" % name)
+            if t.shape[1] < least:
+                raise ValueError("%s has %d bytes in a row, %d columns need %d" % (name, t.shape[1], cols, least))
+            if t.shape[0] > 1 and t.stride(0) < least:
+                raise ValueError("rows of %s must not overlap" % name)
+        if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
+            raise ValueError("codes and scales must have the same rows, on one device")
+        if codes.device.type != "cuda":
+            raise ValueError("microscaled matrices need device tensors; there is no CPU path")
+        self.codes, self.scales, self.format, self.device = codes, scales, format, codes.device
+        self.rows, self.cols = codes.shape[0], cols
+        ld = codes.stride(0) if self.rows > 1 else blocks * _MX_BLOCK_BYTES[format]
+        if self.rows > 0 and cols > 0 and (codes.data_ptr() % 16 or ld % 16):
+            raise ValueError("rows of codes must begin at multiples of 16 bytes")
+        self._record = nt_mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols, ld, scales.stride(0) if self.rows > 1 else blocks, format, 0)
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    def pointer(self):
+        """The library's record of this matrix, as it is now."""
+        self._record.codes, self._record.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        return ctypes.byref(self._record)
+
+
+def make_mx(rows: int, cols: int, format: int = NT_MX_E2M1, device=None) -> MxTensor:
+    """Device memory for a microscaled matrix, to be filled by normtest_mx_quantize or normtest_rms_norm."""
+    if format not in _MX_BLOCK_BYTES:
+        raise ValueError("format must be NT_MX_E2M1 or NT_MX_E4M3, got %r" % (format,))
+    if rows < 0 or cols < 0:
+        raise ValueError("a matrix has no negative sizes, got %d x %d" % (rows, cols))
+    blocks = (cols + _MX_BLOCK - 1) // _MX_BLOCK
+    device = torch.device("cuda" if device is None else device)
+    codes = torch.zeros(rows, blocks * _MX_BLOCK_BYTES[format], dtype=torch.uint8, device=device)
+    return MxTensor(codes, torch.zeros(rows, blocks, dtype=torch.uint8, device=device), cols, format)
+
+
+def _numbers(where: str, name: str, t, shape=None, dtype=None, device=None):
+    """(address, nt_dtype, row stride) of a matrix of numbers."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s: %s must be a 2-D tensor with a contiguous last axis" % (where, name))
+    if t.dtype not in _LIST_DTYPES:
+        raise TypeError("%s: %s must be float32, bfloat16 or float16, got %s" % (where, name, t.dtype))
+    if t.device.type != "cuda":
+        raise ValueError("%s needs device tensors; there is no CPU path" % where)
+    if (shape is not None and tuple(t.shape) != tuple(shape)) or (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
+        raise ValueError("%s: %s must be %s of %s on %s, got %s of %s on %s" % (
+            where, name, "x".join(map(str, shape or t.shape)), dtype or t.dtype, device or t.device, "x".join(map(str, t.shape)), t.dtype, t.device))
+    return t.data_ptr(), _LIST_DTYPES[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _mx(where: str, name: str, m, shape=None, device=None):
+    if not isinstance(m, MxTensor):
+        raise TypeError("%s: %s must be an MxTensor (make_mx), got %s" % (where, name, type(m).__name__))
+    if (shape is not None and m.shape != tuple(shape)) or (device is not None and m.device != device):
+        raise ValueError("%s: %s must be %dx%d on %s, got %dx%d on %s" % (where, name, *(shape or m.shape), device or m.device, *m.shape, m.device))
+    return m.pointer()
+
+
+def _floats(where: str, name: str, t, n: int, device):
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != device or not t.is_contiguous() or t.numel() != n:
+        raise ValueError("%s: %s must be a contiguous float32 tensor of %d elements on %s" % (where, name, n, device))
+    return t.data_ptr()
+
+
+def _scratch(where: str, workspace, need: int, dev, stream):
+    """(workspace, its bytes), made here where the caller has none."""
+    if workspace is None:
+        if not need:
+            return None, 0
+        if _stream_handle(stream, dev) == _stream_handle(None, dev):
+            return torch.empty(need, dtype=torch.uint8, device=dev), need
+        with torch.cuda.stream(stream):   # that stream's memory: what runs on the current one may still use what this one would be given
+            return torch.empty(need, dtype=torch.uint8, device=dev), need
+    if not isinstance(workspace, torch.Tensor) or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("%s: workspace must be contiguous device memory on %s" % (where, dev))
+    return workspace, _nbytes(workspace)
+
+
+def normtest_mx_quantize(src: torch.Tensor, out: Optional[MxTensor] = None, out_t: Optional[MxTensor] = None, *, fit: bool = False,
+                         noise: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Quantise the matrix src (float32, bfloat16 or float16; rows of any stride) into out, its transpose into out_t, or both from one reading.
+
+    A block's scale is the power of two of its largest magnitude, under which that one may be clamped to the format's largest number (6 or
+    448), or with `fit` the least that clamps nothing.  noise: uint8, src's shape; a random byte for every element rounds it up with the
+    probability of its fraction instead of to nearest even.  A block with a NaN or an infinity reads as NaN."""
+    where = "normtest_mx_quantize"
+    address, dtype, ld = _numbers(where, "src", src)
+    (rows, cols), dev = src.shape, src.device
+    if out is None and out_t is None:
+        raise ValueError("%s needs out, out_t or both" % where)
+    if noise is not None and (not isinstance(noise, torch.Tensor) or noise.dtype != torch.uint8 or noise.shape != src.shape or noise.device != dev
+                              or (cols > 1 and noise.stride(1) != 1)):
+        raise ValueError("%s: noise must be a uint8 tensor of src's shape on %s with a contiguous last axis" % (where, dev))
+    rc = _call(dev, lib().normtest_mx_quantize, address, dtype, rows, cols, ld, _ptr(noise),
+               0 if noise is None else noise.stride(0) if rows > 1 else cols, None if out is None else _mx(where, "out", out, (rows, cols), dev),
+               None if out_t is None else _mx(where, "out_t", out_t, (cols, rows), dev), NT_MX_FIT if fit else 0, _stream_handle(stream, dev))
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
+
+
+def normtest_mx_dequantize(src: MxTensor, out: Optional[torch.Tensor] = None, *, dtype: torch.dtype = torch.bfloat16,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The numbers that src stands for, into out (any of the three types) or a new matrix of `dtype`."""
+    where = "normtest_mx_dequantize"
+    record = _mx(where, "src", src)
+    if out is None:
+        out = _fresh(src.shape, dtype, src.device, stream)
+    address, kind, ld = _numbers(where, "out", out, src.shape, None, src.device)
+    rc = _call(src.device, lib().normtest_mx_dequantize, record, address, kind, ld, _stream_handle(stream, src.device))
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
+    return out
+
+
+def _fresh(shape, dtype, dev, stream) -> torch.Tensor:
+    """A new result: memory of the stream that writes it, which the current one may read once it has waited for that stream."""
+    if _stream_handle(stream, dev) == _stream_handle(None, dev):
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    out.record_stream(torch.cuda.current_stream(dev))
+    return out
+
+
+def normtest_mx_matmul_workspace_bytes(a: MxTensor, b: MxTensor, dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes that normtest_mx_matmul(a, b) into a result of this type works in; often 0."""
+    return int(lib().normtest_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols, a.format, b.format, _LIST_DTYPES[dtype]))
+
+
+def normtest_mx_matmul(a: MxTensor, b: MxTensor, out: Optional[torch.Tensor] = None, *, dtype: torch.dtype = torch.bfloat16, scale: float = 1.0,
+                       beta: float = 0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """out <- beta out + scale a b^T (a: M x K, b: N x K, of any formats; out: M x N, rows of any stride, or a new matrix of `dtype`).
+
+    A weight's gradient with beta = 1 and a row of the norm test as out is accumulated there.  workspace: device memory of
+    normtest_mx_matmul_workspace_bytes(a, b, out.dtype) bytes; made here if it is not given."""
+    where = "normtest_mx_matmul"
+    pa, pb = _mx(where, "a", a), _mx(where, "b", b)
+    dev = a.device
+    if b.device != dev or a.cols != b.cols:
+        raise ValueError("%s: a and b must have the same columns, on one device: got %dx%d on %s and %dx%d on %s" % (where, *a.shape, dev, *b.shape, b.device))
+    if out is None:
+        if beta != 0.0:
+            raise ValueError("%s: beta needs an out to read" % where)
+        if dtype not in _LIST_DTYPES:
+            raise TypeError("%s: dtype must be float32, bfloat16 or float16, got %s" % (where, dtype))
+        out = _fresh((a.rows, b.rows), dtype, dev, stream)
+    address, kind, ld = _numbers(where, "out", out, (a.rows, b.rows), None, dev)
+    own = workspace is None
+    workspace, size = _scratch(where, workspace, normtest_mx_matmul_workspace_bytes(a, b, out.dtype) if own else 0, dev, stream)
+    rc = _call(dev, lib().normtest_mx_matmul, pa, pb, float(scale), float(beta), address, kind, ld, _ptr(workspace), size, _stream_handle(stream, dev))
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
+    return out
+
+
+def normtest_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], out: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
+                      eps: float = 1e-5, sum_out: Optional[torch.Tensor] = None, out_mx: Optional[MxTensor] = None,
+                      rstd: Optional[torch.Tensor] = None, fit: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """h = x + residual (stored to sum_out in x's type), rstd = 1 / sqrt(mean(h^2) + eps) per row (float32), and h rstd weight into out (x's
+    type), out_mx (codes and scales, `fit` as in normtest_mx_quantize) or both.  Everything but x may be left out; sum_out may be x or residual."""
+    where = "normtest_rms_norm"
+    px, kind, x_ld = _numbers(where, "x", x)
+    (rows, cols), dev = x.shape, x.device
+    pr, _, r_ld = (None, 0, 0) if residual is None else _numbers(where, "residual", residual, x.shape, x.dtype, dev)
+    ps, _, s_ld = (None, 0, 0) if sum_out is None else _numbers(where, "sum_out", sum_out, x.shape, x.dtype, dev)
+    po, _, o_ld = (None, 0, 0) if out is None else _numbers(where, "out", out, x.shape, x.dtype, dev)
+    rc = _call(dev, lib().normtest_rms_norm, px, x_ld, pr, r_ld, _floats(where, "weight", weight, cols, dev), float(eps), kind, rows, cols, ps, s_ld,
+               po, o_ld, None if out_mx is None else _mx(where, "out_mx", out_mx, x.shape, dev), _floats(where, "rstd", rstd, rows, dev),
+               NT_MX_FIT if fit else 0, _stream_handle(stream, dev))
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
+
+
+def normtest_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().normtest_rms_norm_workspace_bytes(rows, cols))
+
+
+def normtest_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor,
+                               dx: Optional[torch.Tensor] = None, *, dsum: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                               scale: float = 1.0, beta: float = 0.0, workspace: Optional[torch.Tensor] = None,
+                               stream: Optional[torch.cuda.Stream] = None) -> None:
+    """From dy, the gradient of the norm's output, and the forward pass's sum h, weight and rstd: dx, the gradient of x and of the residual,
+    dsum (what else comes back to h) included, and dweight <- beta dweight + scale (its gradient), float32.  dx may be dy or dsum.
+    workspace: device memory of normtest_rms_norm_workspace_bytes(rows, cols) bytes for dweight; made here if it is not given."""
+    where = "normtest_rms_norm_backward"
+    py, kind, y_ld = _numbers(where, "dy", dy)
+    (rows, cols), dev = dy.shape, dy.device
+    ph, _, h_ld = _numbers(where, "h", h, dy.shape, dy.dtype, dev)
+    ps, _, s_ld = (None, 0, 0) if dsum is None else _numbers(where, "dsum", dsum, dy.shape, dy.dtype, dev)
+    px, _, x_ld = (None, 0, 0) if dx is None else _numbers(where, "dx", dx, dy.shape, dy.dtype, dev)
+    if dx is None and dweight is None:
+        raise ValueError("%s needs dx, dweight or both" % where)
+    own = workspace is None
+    workspace, size = _scratch(where, workspace, normtest_rms_norm_workspace_bytes(rows, cols) if own and dweight is not None else 0, dev, stream)
+    rc = _call(dev, lib().normtest_rms_norm_backward, py, y_ld, ph, h_ld, _floats(where, "weight", weight, cols, dev),
+               _floats(where, "rstd", rstd, rows, dev), ps, s_ld, kind, rows, cols, px, x_ld, _floats(where, "dweight", dweight, cols, dev),
+               float(scale), float(beta), _ptr(workspace), size, _stream_handle(stream, dev))
+    if rc != NT_OK:
+        raise NormtestError(rc, where)
 
 
 def normtest_clip_coef(gbar_sq: float, max_norm: float) -> float:

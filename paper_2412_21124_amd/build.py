@@ -1,5 +1,5 @@
-"""Build ``libnormtest.so`` from ``csrc/normtest.hip`` and ``csrc/tensors.hip`` for gfx950 with hipcc (works without a GPU), and the
-binding's native call path from ``csrc/callpath.cpp`` with g++."""
+"""Build ``libnormtest.so`` from the sources ``csrc/*.hip`` for gfx950 with hipcc (works without a GPU), and the binding's native call
+path from ``csrc/callpath.cpp`` with g++."""
 from __future__ import annotations
 
 import os
@@ -10,6 +10,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "normtest.hip")
 TENSORS_SRC = os.path.join(_HERE, "csrc", "tensors.hip")
+MX_SRC = os.path.join(_HERE, "csrc", "mx.hip")
+MX_MATMUL_SRC = os.path.join(_HERE, "csrc", "mx_matmul.hip")
+MX_HEADER = os.path.join(_HERE, "csrc", "mx.h")
 LIB = os.path.join(_HERE, "libnormtest.so")
 INCLUDE = os.path.join(ROOT, "include")
 CALLPATH_SRC = os.path.join(_HERE, "csrc", "callpath.cpp")
@@ -24,10 +27,10 @@ HIPCC_FLAGS = [
 
 
 def build_library(out: str = LIB, quiet: bool = True) -> str:
-    """Both sources at the same time, each to an object of its own, then the library."""
+    """The sources at the same time, each to an object of its own, then the library."""
     tmp = out + ".tmp.%d" % os.getpid()
     objects, running = [], []
-    for src in (SRC, TENSORS_SRC):
+    for src in (SRC, TENSORS_SRC, MX_SRC, MX_MATMUL_SRC):
         objects.append("%s.%s.o" % (tmp, os.path.splitext(os.path.basename(src))[0]))
         running.append(_start(["hipcc", *HIPCC_FLAGS, "-I", INCLUDE, "-c", "-o", objects[-1], src]))
     try:
@@ -85,7 +88,7 @@ def _stale(built: str, *sources: str) -> bool:
 def ensure_built() -> str:
     """Path of the built library; builds it if nothing is there or a source is newer than the build."""
     header = os.path.join(INCLUDE, "normtest.h")
-    if _stale(LIB, SRC, TENSORS_SRC, header):
+    if _stale(LIB, SRC, TENSORS_SRC, MX_SRC, MX_MATMUL_SRC, MX_HEADER, header):
         build_library()
     return LIB
 
