@@ -14,6 +14,11 @@
 #define NT_MM_CHUNK 512            // columns that a wave takes at a time: 16 blocks, four for a lane
 #define NT_MM_CHUNK_BLOCKS 16
 #define NT_MM_THIN_WAVES 4
+#ifndef NT_MM_LM
+#define NT_MM_LM 2
+#define NT_MM_LN 4
+#endif
+#define NT_MM_TILE_LD (1ll << 22)   // bytes from row to row that 32-bit offsets into a tile allow
 
 namespace {
 
@@ -45,17 +50,44 @@ __device__ inline float read_as(int dtype, const char* p) {
 }
 // n <= 4 results of row m from column `col` on
 __device__ inline void put4(const MatmulArgs& a, int64_t m, int64_t col, f32x4 x, int n) {
+  typedef uint32_t u32x2_half __attribute__((ext_vector_type(2), aligned(2)));
   if (a.parts) {
     float* const to = a.parts + m * a.b.rows + col;
-    for (int i = 0; i < 4; ++i)
-      if (i < n) to[i] = x[i];
+    if (n == 4) {
+      *(u32x4_word*)to = __builtin_bit_cast(u32x4, x);
+    } else {
+      for (int i = 0; i < 3; ++i)
+        if (i < n) to[i] = x[i];
+    }
     return;
   }
   char* const to = a.out + (m * a.ld + col) * type_bytes(a.dtype);
-  for (int i = 0; i < 4; ++i)
+  x *= a.scale;
+  if (n == 4) {
+    if (a.dtype == NT_F32) {
+      if (a.beta != 0.f) {
+        const f32x4 old = __builtin_bit_cast(f32x4, (u32x4) * (const u32x4_word*)to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(a.beta, old[i], x[i]);
+      }
+      *(u32x4_word*)to = __builtin_bit_cast(u32x4, x);
+    } else {
+      if (a.beta != 0.f) {
+        const u32x2 old = *(const u32x2_half*)to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint16_t h = (uint16_t)(old[i >> 1] >> (16 * (i & 1)));
+          x[i] = __builtin_fmaf(a.beta, a.dtype == NT_BF16 ? __builtin_bit_cast(float, (uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h), x[i]);
+        }
+      }
+      *(u32x2_half*)to = u32x2{half_bits(a.dtype, x[0]) | half_bits(a.dtype, x[1]) << 16, half_bits(a.dtype, x[2]) | half_bits(a.dtype, x[3]) << 16};
+    }
+    return;
+  }
+  for (int i = 0; i < 3; ++i)
     if (i < n) {
       char* const p = to + i * type_bytes(a.dtype);
-      float y = x[i] * a.scale;
+      float y = x[i];
       if (a.beta != 0.f) y = __builtin_fmaf(a.beta, read_as(a.dtype, p), y);
       if (a.dtype == NT_F32)
         *(float*)p = y;
@@ -215,24 +247,275 @@ __global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------
+// Tiles
+// ---------------------------------------------------------------------------------------------
+// A block takes BM x BN of the result.  Steps of 256 (4 bits both) or 128 columns of A and B go from memory to LDS without passing
+// registers, into one half while the other is multiplied; a chunk's scales, 16 bytes a row, go through registers, where their
+// bytes are transposed, so that lane (r, g) reads the four scales that it needs for the chunk's four instructions as one word.
+// A row of LDS has 64 or 128 bytes without a gap (what goes there directly lies as the lanes do), so 16-byte pieces of neighbouring rows change places
+// by the row's number: 16 lanes that read one piece of 16 rows then meet all banks.
+template <int FA, int FB>
+constexpr int step_columns() {
+  return FA == NT_MX_E2M1 && FB == NT_MX_E2M1 ? 256 : 128;
+}
+template <int F>
+constexpr int row_bytes(int columns) {
+  return F == NT_MX_E2M1 ? columns / 2 : columns;
+}
+template <int BYTES>   // of a row
+__device__ inline int swapped(int row, int piece) {
+  return BYTES == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
+}
+
+// 16 bytes a lane from memory to consecutive bytes of LDS.  What lies beyond the descriptor's size reads as zeros.  The compiler does not know
+// of these loads: whoever reads the LDS waits for them by landed().
+__device__ inline void to_lds(u32x4 from, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(from), "s"(to) : "memory", "m0");
+}
+// all loads of this wave have arrived, all its LDS accesses are done, and every other wave of the block is here too
+__device__ inline void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+// A tile's rows of one operand, a step of columns at a time.  What moves, from row to row and from step to step, moves the descriptor, on the scalar
+// unit: one offset a lane serves all loads.  (With an offset for each, spilled registers were read back between the loads, and each waited for the last.)
+template <int F, int TILE, int COLUMNS, int WAVES>
+struct Loader {
+  static constexpr int BYTES = row_bytes<F>(COLUMNS), PIECES = BYTES / 16, ROWS = 64 / PIECES, TURNS = TILE / (ROWS * WAVES);
+  static_assert(TURNS * ROWS * WAVES == TILE, "whole turns");
+  uint64_t at;
+  int32_t size, turn;          // turn: bytes from one of a wave's loads to the next
+  uint32_t wave;
+  uint32_t offset, piece;      // of this lane; piece: bytes into the step
+  __device__ inline void init(const Operand& o, int64_t row0, int64_t block0, int64_t blocks) {
+    const int lane = threadIdx.x & 63;
+    wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int row = (int)wave * ROWS + lane / PIECES;
+    const int64_t rows = o.rows - row0 < TILE ? o.rows - row0 : TILE;
+    at = (uint64_t)(uintptr_t)(o.codes + row0 * o.ld + block0 * code_bytes(F));
+    size = (int32_t)((rows - 1) * o.ld + (blocks - block0) * code_bytes(F));
+    piece = (uint32_t)swapped<BYTES>(row, lane % PIECES) * 16;
+    offset = (uint32_t)row * (uint32_t)o.ld + piece;
+    turn = ROWS * WAVES * (int32_t)o.ld;
+  }
+  // left: bytes of a row from this step on; none or fewer: zeros
+  __device__ inline void step(uint32_t to, int32_t left) {
+    const uint32_t off = (int32_t)piece < left ? offset : 0x80000000u;   // behind the row's last block: beyond the descriptor's size too
+    uint64_t from = at;
+    int32_t here = size;
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+      to_lds(u32x4{(uint32_t)from, (uint32_t)(from >> 32), (uint32_t)here, 0x00020000u}, off, to + (uint32_t)(i * WAVES * 1024) + wave * 1024u);
+      from += (uint32_t)turn;
+      here = here - turn > 0 ? here - turn : 0;
+    }
+    at += BYTES;
+    size = size - BYTES > 0 ? size - BYTES : 0;
+  }
+};
+
+// rows of 16 scale bytes to words by lane group
+__device__ inline u32x4 by_group(const u32x4& w) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);   // 0 0' 1 1', 2 2' 3 3'
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  return u32x4{__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u), __builtin_amdgcn_perm(d, b, 0x05040100u),
+               __builtin_amdgcn_perm(d, b, 0x07060302u)};
+}
+__device__ inline u32x4 load_scales(const Operand& o, int64_t row, int64_t block0, int64_t blocks) {
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (row >= o.rows) return w;
+  const uint8_t* const p = o.scales + row * o.scale_ld + block0;
+  if (block0 + 16 <= blocks) return *(const u32x4_byte*)p;
+  for (int i = 0; i < (int)(blocks - block0); ++i) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  return w;
+}
+
+template <int FA, int FB, bool WIDE, int BM, int BN, int WM, int WN>
+struct TileShape {
+  static constexpr int THREADS = 64 * WM * WN, STEP = step_columns<FA, FB>(), STEPS = NT_MM_CHUNK / STEP;
+  static constexpr int A_BYTES = BM * row_bytes<FA>(STEP), B_BYTES = BN * row_bytes<FB>(STEP), STAGE = A_BYTES + B_BYTES;
+  static constexpr int SCALES = 2 * STAGE, LDS = SCALES + 2 * 16 * (BM + BN);
+};
+
+template <int FA, int FB, bool WIDE, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t down, uint32_t across, int32_t chunks_each) {
+  typedef TileShape<FA, FB, WIDE, BM, BN, WM, WN> S;
+  extern __shared__ __align__(1024) uint8_t lds[];
+  constexpr int MT = BM / WM / 16, NT = BN / WN / 16, RA = row_bytes<FA>(S::STEP), RB = row_bytes<FB>(S::STEP), WAVES = WM * WN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+
+  // Tiles are numbered so that the blocks that one of the eight dies is given (every eighth) are neighbours: 8 rows of tiles at a time.
+  uint32_t t = blockIdx.x;
+  {
+    const uint32_t total = gridDim.x, each = total / 8, more = total % 8, die = t % 8;
+    t = t / 8 + die * each + (die < more ? die : more);
+  }
+  const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8;
+  const uint32_t in = t - group * 8 * across;
+  const int64_t m0 = (int64_t)(first + in % high) * BM, n0 = (int64_t)(in / high) * BN;
+
+  const int64_t chunk0 = (int64_t)blockIdx.y * chunks_each, block0 = chunk0 * NT_MM_CHUNK_BLOCKS;
+  const int64_t end = (chunk0 + chunks_each) * NT_MM_CHUNK_BLOCKS, blocks = end < a.blocks ? end : a.blocks;   // of this part of the columns
+  const int steps = (int)((blocks - block0 + S::STEP / 32 - 1) / (S::STEP / 32));
+
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  Loader<FA, BM, S::STEP, WAVES> la;
+  Loader<FB, BN, S::STEP, WAVES> lb;
+  la.init(a.a, m0, block0, blocks);
+  lb.init(a.b, n0, block0, blocks);
+  auto load = [&](int step) {
+    const int32_t left = (int32_t)(blocks - block0) - step * (S::STEP / 32);
+    const uint32_t to = base + (uint32_t)(step & 1) * S::STAGE;
+    la.step(to, left * code_bytes(FA));
+    lb.step(to + S::A_BYTES, left * code_bytes(FB));
+  };
+  constexpr int SCALE_TURNS = (BM + BN + S::THREADS - 1) / S::THREADS;
+  u32x4 scales[SCALE_TURNS];
+  auto fetch = [&](int64_t block) {
+#pragma unroll
+    for (int i = 0; i < SCALE_TURNS; ++i) {
+      const int row = i * S::THREADS + (int)threadIdx.x;
+      if (row < BM + BN) scales[i] = row < BM ? load_scales(a.a, m0 + row, block, blocks) : load_scales(a.b, n0 + row - BM, block, blocks);
+    }
+  };
+  auto keep = [&](int chunk) {
+#pragma unroll
+    for (int i = 0; i < SCALE_TURNS; ++i) {
+      const int row = i * S::THREADS + (int)threadIdx.x;
+      if (row < BM + BN) *(u32x4*)(lds + S::SCALES + (chunk & 1) * 16 * (BM + BN) + 16 * row) = by_group(scales[i]);
+    }
+  };
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // where this lane's pieces are in a stage: rows 16 apart have their pieces in the same order
+  constexpr int PARTS = S::STEP / 128;
+  int at_a[PARTS][2], at_b[PARTS][2];
+#pragma unroll
+  for (int u = 0; u < PARTS; ++u)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int ia = FA == NT_MX_E2M1 ? 4 * u + g : WIDE ? 2 * g + h : 4 * h + g, ib = FB == NT_MX_E2M1 ? 4 * u + g : WIDE ? 2 * g + h : 4 * h + g;
+      at_a[u][h] = (wm + r) * RA + swapped<RA>(r, ia) * 16;
+      at_b[u][h] = S::A_BYTES + (wn + r) * RB + swapped<RB>(r, ib) * 16;
+    }
+
+  fetch(block0);
+  load(0);
+  keep(0);
+  landed();
+
+  uint32_t sa[MT], sb[NT];
+  for (int at = 0; at < steps; ++at) {
+    const int chunk = at / S::STEPS;
+    const int64_t next = block0 + (int64_t)(chunk + 1) * NT_MM_CHUNK_BLOCKS;
+    if (at % S::STEPS == 0) {
+      const uint8_t* const ps = lds + S::SCALES + (chunk & 1) * 16 * (BM + BN) + 4 * g;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sa[i] = *(const uint32_t*)(ps + 16 * (wm + 16 * i + r));
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sb[j] = *(const uint32_t*)(ps + 16 * (BM + wn + 16 * j + r));
+      if (next < blocks) fetch(next);
+    }
+    load(at + 1);   // zeros behind the last one
+    const uint8_t* const stage = lds + (at & 1) * S::STAGE;
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      if (u) __builtin_amdgcn_sched_barrier(0);   // its fragments in the registers of the part before
+      Frag<FA> fa[MT];
+      Frag<FB> fb[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        fb[j].w[0] = *(const u32x4*)(stage + at_b[u][0] + 16 * j * RB);
+        if (FB == NT_MX_E4M3) fb[j].w[FB == NT_MX_E4M3] = *(const u32x4*)(stage + at_b[u][1] + 16 * j * RB);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        fa[i].w[0] = *(const u32x4*)(stage + at_a[u][0] + 16 * i * RA);
+        if (FA == NT_MX_E4M3) fa[i].w[FA == NT_MX_E4M3] = *(const u32x4*)(stage + at_a[u][1] + 16 * i * RA);
+      }
+      if constexpr (!WIDE) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[i][j] = u == 0 ? multiply<FA, FB, 0>(fb[j], sb[j], fa[i], sa[i], acc[i][j]) : multiply<FA, FB, 1>(fb[j], sb[j], fa[i], sa[i], acc[i][j]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          bf16x8 x[MT];
+#pragma unroll
+          for (int i = 0; i < MT; ++i) x[i] = widened<FA>(fa[i], p, grow(sa[i] & 255u));
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const bf16x8 y = widened<FB>(fb[j], p, grow(sb[j] & 255u));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[i], acc[i][j], 0, 0, 0);
+          }
+        }
+      }
+    }
+    // the next step's scales come down to the lowest bytes
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[i] >>= 8 * PARTS;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sb[j] >>= 8 * PARTS;
+    if (at % S::STEPS == S::STEPS - 1 && next < blocks) keep(chunk + 1);
+    landed();
+  }
+
+  if (gridDim.y > 1) a.parts += (int64_t)blockIdx.y * a.a.rows * a.b.rows;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + wm + 16 * i + r;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int64_t col = n0 + wn + 16 * j + 4 * g, left = a.b.rows - col;
+      if (m < a.a.rows && left > 0) put4(a, m, col, acc[i][j], left < 4 ? (int)left : 4);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
+enum { THIN, MIDDLE, LARGE };
 struct MatmulPlan {
   bool wide;
-  int rows;      // 16-row groups of a wave
-  int splits;
-  dim3 grid;
+  int kind, rows;        // rows: THIN: 16-row groups of a wave
+  uint32_t down, across; // tiles
+  int splits, chunks;    // parts of the columns, and chunks of 512 in each
 };
-MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype) {
+MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, int64_t ld) {
   MatmulPlan p;
   p.wide = dtype == NT_F32 && (fa == NT_MX_E4M3 || fb == NT_MX_E4M3);
+  const int64_t chunks = ceil_div(K, NT_MM_CHUNK);
   p.rows = M <= 16 ? 1 : 2;
-  const int64_t across = ceil_div(N, 16), down = ceil_div(M, 16 * p.rows), turns = ceil_div(ceil_div(K, NT_MM_CHUNK), NT_MM_THIN_WAVES);
   int64_t z = 1;
-  if (across * down < 256) z = ceil_div(512, across * down);
-  if (z > turns) z = turns;
-  p.splits = z < 1 ? 1 : (int)z;
-  p.grid = dim3((uint32_t)across, (uint32_t)down, (uint32_t)p.splits);
+  if (M <= 32 || ld > NT_MM_TILE_LD) {
+    p.kind = THIN;
+    p.across = (uint32_t)ceil_div(N, 16);
+    p.down = (uint32_t)ceil_div(M, 16 * p.rows);
+    const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(chunks, NT_MM_THIN_WAVES);
+    if (tiles < 256) z = ceil_div(512, tiles);
+    if (z > turns) z = turns;
+    p.chunks = 0;
+  } else {
+    p.kind = !p.wide && ceil_div(M, 256) * ceil_div(N, 256) >= 192 ? LARGE : MIDDLE;
+    const int tile = p.kind == LARGE ? 256 : 128;
+    p.down = (uint32_t)ceil_div(M, tile);
+    p.across = (uint32_t)ceil_div(N, tile);
+    const int64_t tiles = (int64_t)p.across * p.down;
+    if (tiles < 256) z = 512 / tiles;
+    if (z > chunks / 2) z = chunks / 2;
+    if (z < 1) z = 1;
+    p.chunks = (int)ceil_div(chunks, z);
+    z = ceil_div(chunks, p.chunks);
+  }
+  p.splits = (int)z;
   return p;
 }
 template <class F>
@@ -258,7 +541,7 @@ extern "C" {
 
 size_t normtest_mx_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, nt_mx_format a, nt_mx_format b, nt_dtype dtype) {
   if (M <= 0 || N <= 0 || K <= 0) return 0;
-  const MatmulPlan p = plan_of(M, N, K, a, b, dtype);
+  const MatmulPlan p = plan_of(M, N, K, a, b, dtype, 0);
   return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
 
@@ -281,23 +564,31 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
     hipLaunchKernelGGL(k_mm_empty, dim3(grid_of(M * N)), dim3(256), 0, st, args);
     return hip_code(hipGetLastError());
   }
-  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype);
+  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype, a->ld > b->ld ? a->ld : b->ld);
   if (p.splits > 1) {
-    if (!workspace || workspace_bytes < normtest_mx_matmul_workspace_bytes(M, N, K, (nt_mx_format)a->format, (nt_mx_format)b->format, dtype))
-      return NT_ERR_WORKSPACE_TOO_SMALL;
+    if (!workspace || workspace_bytes < (size_t)p.splits * (size_t)M * (size_t)N * sizeof(float)) return NT_ERR_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace & 15) return NT_ERR_BAD_ARG;
     args.parts = (float*)workspace;
   }
   rc = with_format(a->format, [&](auto fa) {
     return with_format(b->format, [&](auto fb) {
-      auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, p.grid, dim3(64 * NT_MM_THIN_WAVES), 0, st, args);
-        return hip_code(hipGetLastError());
-      };
       constexpr int A = decltype(fa)::value, B = decltype(fb)::value;
       constexpr bool W = A == NT_MX_E4M3 || B == NT_MX_E4M3;
-      if (p.wide) return p.rows == 1 ? launch(k_mm_thin<A, B, W, 1>) : launch(k_mm_thin<A, B, W, 2>);
-      return p.rows == 1 ? launch(k_mm_thin<A, B, false, 1>) : launch(k_mm_thin<A, B, false, 2>);
+      auto thin = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(p.across, p.down, (uint32_t)p.splits), dim3(64 * NT_MM_THIN_WAVES), 0, st, args);
+        return hip_code(hipGetLastError());
+      };
+      auto tile = [&](auto kernel, int threads, int lds) {
+        hipLaunchKernelGGL(kernel, dim3(p.down * p.across, (uint32_t)p.splits), dim3(threads), lds, st, args, p.down, p.across, p.chunks);
+        return hip_code(hipGetLastError());
+      };
+      if (p.kind == THIN) {
+        if (p.wide) return p.rows == 1 ? thin(k_mm_thin<A, B, W, 1>) : thin(k_mm_thin<A, B, W, 2>);
+        return p.rows == 1 ? thin(k_mm_thin<A, B, false, 1>) : thin(k_mm_thin<A, B, false, 2>);
+      }
+      if (p.kind == LARGE) return tile(k_mm_tile<A, B, false, 256, 256, NT_MM_LM, NT_MM_LN>, 64 * NT_MM_LM * NT_MM_LN, TileShape<A, B, false, 256, 256, NT_MM_LM, NT_MM_LN>::LDS);
+      if (p.wide) return tile(k_mm_tile<A, B, W, 128, 128, 2, 2>, 256, TileShape<A, B, W, 128, 128, 2, 2>::LDS);
+      return tile(k_mm_tile<A, B, false, 128, 128, 2, 2>, 256, TileShape<A, B, false, 128, 128, 2, 2>::LDS);
     });
   });
   if (rc != NT_OK || p.splits == 1) return rc;

@@ -227,7 +227,8 @@ def test_product_scales(form, form_b):
 @pytest.mark.parametrize("form,form_b", KINDS, ids="-".join)
 def test_product_of_many_tiles(form, form_b):
     """More tiles than the chip takes at once, edges that end inside one, and sums over parts of the columns: against a product in 64 bits on the GPU."""
-    for M, N, K, dtype in ((1000, 2100, 300, "bf16"), (700, 900, 5000, "f32"), (64, 128, 40000, "f32"), (2, 40, 70000, "bf16"), (520, 1030, 1500, "f16")):
+    for M, N, K, dtype in ((1000, 2100, 300, "bf16"), (700, 900, 5000, "f32"), (64, 128, 40000, "f32"), (2, 40, 70000, "bf16"), (520, 1030, 1500, "f16"),
+                           (3700, 3700, 700, "bf16")):
         a, b = operand(M, K, form, M), operand(N, K, form_b, N)
         na, nb = torch.from_numpy(R.numbers(a)).to(DEV), torch.from_numpy(R.numbers(b)).to(DEV)
         want = na @ nb.t().contiguous()
