@@ -896,7 +896,8 @@ def make_mx(rows: int, cols: int, format: int = NT_MX_E2M1, device=None) -> MxTe
     blocks = (cols + _MX_BLOCK - 1) // _MX_BLOCK
     device = torch.device("cuda" if device is None else device)
     codes = torch.zeros(rows, blocks * _MX_BLOCK_BYTES[format], dtype=torch.uint8, device=device)
-    return MxTensor(codes, torch.zeros(rows, blocks, dtype=torch.uint8, device=device), cols, format)
+    # rows of scales at multiples of 16 bytes, as the product of large matrices wants them
+    return MxTensor(codes, torch.zeros(rows, (blocks + 15) // 16 * 16, dtype=torch.uint8, device=device), cols, format)
 
 
 def _numbers(where: str, name: str, t, shape=None, dtype=None, device=None):

@@ -14,10 +14,6 @@
 #define NT_MM_CHUNK 512            // columns that a wave takes at a time: 16 blocks, four for a lane
 #define NT_MM_CHUNK_BLOCKS 16
 #define NT_MM_THIN_WAVES 4
-#ifndef NT_MM_LM
-#define NT_MM_LM 2
-#define NT_MM_LN 4
-#endif
 #define NT_MM_TILE_LD (1ll << 22)   // bytes from row to row that 32-bit offsets into a tile allow
 
 namespace {
@@ -264,7 +260,7 @@ constexpr int row_bytes(int columns) {
 }
 template <int BYTES>   // of a row
 __device__ inline int swapped(int row, int piece) {
-  return BYTES == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
+  return piece ^ ((row >> 1) & (BYTES / 16 - 1));
 }
 
 // 16 bytes a lane from memory to consecutive bytes of LDS.  What lies beyond the descriptor's size reads as zeros.  The compiler does not know
@@ -282,7 +278,7 @@ struct Loader {
   static constexpr int BYTES = row_bytes<F>(COLUMNS), PIECES = BYTES / 16, ROWS = 64 / PIECES, TURNS = TILE / (ROWS * WAVES);
   static_assert(TURNS * ROWS * WAVES == TILE, "whole turns");
   uint64_t at;
-  int32_t size, turn;          // turn: bytes from one of a wave's loads to the next
+  int32_t size, turn;          // turn: bytes from one of a wave's loads to the next; size: none left where it is not positive
   uint32_t wave;
   uint32_t offset, piece;      // of this lane; piece: bytes into the step
   __device__ inline void init(const Operand& o, int64_t row0, int64_t block0, int64_t blocks) {
@@ -296,19 +292,21 @@ struct Loader {
     offset = (uint32_t)row * (uint32_t)o.ld + piece;
     turn = ROWS * WAVES * (int32_t)o.ld;
   }
-  // left: bytes of a row from this step on; none or fewer: zeros
-  __device__ inline void step(uint32_t to, int32_t left) {
+  // One of the step's loads.  left: bytes of a row from this step on; none or fewer: zeros.
+  __device__ inline void load(uint32_t to, int32_t left, int i) const {
     const uint32_t off = (int32_t)piece < left ? offset : 0x80000000u;   // behind the row's last block: beyond the descriptor's size too
-    uint64_t from = at;
-    int32_t here = size;
-#pragma unroll
-    for (int i = 0; i < TURNS; ++i) {
-      to_lds(u32x4{(uint32_t)from, (uint32_t)(from >> 32), (uint32_t)here, 0x00020000u}, off, to + (uint32_t)(i * WAVES * 1024) + wave * 1024u);
-      from += (uint32_t)turn;
-      here = here - turn > 0 ? here - turn : 0;
-    }
+    const uint64_t from = at + (uint64_t)(uint32_t)(i * turn);
+    const int32_t here = size - i * turn;
+    to_lds(u32x4{(uint32_t)from, (uint32_t)(from >> 32), (uint32_t)(here > 0 ? here : 0), 0x00020000u}, off, to + (uint32_t)(i * WAVES * 1024) + wave * 1024u);
+  }
+  __device__ inline void next() {
     at += BYTES;
-    size = size - BYTES > 0 ? size - BYTES : 0;
+    size -= BYTES;
+  }
+  __device__ inline void step(uint32_t to, int32_t left) {
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) load(to, left, i);
+    next();
   }
 };
 
@@ -328,6 +326,15 @@ __device__ inline u32x4 load_scales(const Operand& o, int64_t row, int64_t block
   return w;
 }
 
+// Which tile a block takes: numbered so that the blocks that one of the eight dies is given (every eighth) are neighbours, 8 rows of tiles at a time.
+__device__ inline void tile_at(uint32_t down, uint32_t across, int64_t& m, int64_t& n) {
+  const uint32_t total = gridDim.x, each = total / 8, more = total % 8, die = blockIdx.x % 8;
+  const uint32_t t = blockIdx.x / 8 + die * each + (die < more ? die : more);
+  const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8, in = t - group * 8 * across;
+  m = first + in % high;
+  n = in / high;
+}
+
 template <int FA, int FB, bool WIDE, int BM, int BN, int WM, int WN>
 struct TileShape {
   static constexpr int THREADS = 64 * WM * WN, STEP = step_columns<FA, FB>(), STEPS = NT_MM_CHUNK / STEP;
@@ -343,16 +350,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
 
-  // Tiles are numbered so that the blocks that one of the eight dies is given (every eighth) are neighbours: 8 rows of tiles at a time.
-  uint32_t t = blockIdx.x;
-  {
-    const uint32_t total = gridDim.x, each = total / 8, more = total % 8, die = t % 8;
-    t = t / 8 + die * each + (die < more ? die : more);
-  }
-  const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8;
-  const uint32_t in = t - group * 8 * across;
-  const int64_t m0 = (int64_t)(first + in % high) * BM, n0 = (int64_t)(in / high) * BN;
-
+  int64_t m0, n0;
+  tile_at(down, across, m0, n0);
+  m0 *= BM;
+  n0 *= BN;
   const int64_t chunk0 = (int64_t)blockIdx.y * chunks_each, block0 = chunk0 * NT_MM_CHUNK_BLOCKS;
   const int64_t end = (chunk0 + chunks_each) * NT_MM_CHUNK_BLOCKS, blocks = end < a.blocks ? end : a.blocks;   // of this part of the columns
   const int steps = (int)((blocks - block0 + S::STEP / 32 - 1) / (S::STEP / 32));
@@ -479,6 +480,170 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t
   }
 }
 
+// The same for many tiles: 256 x 256 by eight waves, one block to a CU, steps of 128 columns in a ring of two to four stages, all but one of which are
+// on their way.  Scales, 16 bytes a row for four steps, go to LDS directly too, which asks for rows of scales at multiples of 16 bytes.
+template <int FA, int FB>
+struct LargeShape {
+  static constexpr int TILE = 256, WM = 2, WN = 4, WAVES = WM * WN, THREADS = 64 * WAVES, STEP = 128, STEPS = NT_MM_CHUNK / STEP;
+  static constexpr int RA = row_bytes<FA>(STEP), RB = row_bytes<FB>(STEP), A_BYTES = TILE * RA, STAGE = TILE * (RA + RB);
+  static constexpr int SCALES = 2 * TILE * 16;   // of a chunk; two of them
+  static constexpr int FIT = (163840 - 2 * SCALES) / STAGE, STAGES = FIT > 4 ? 4 : FIT, LDS = STAGES * STAGE + 2 * SCALES;
+};
+__device__ inline uint64_t scalar(uint64_t x) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+}
+// waits until at most N of this wave's loads are on their way, and for the block
+template <int N>
+__device__ inline void landed_but() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+}
+
+// Lane (r, g) has the scales of blocks 4 g .. 4 g + 3 of a row, and gets those of the blocks g, 4 + g, 8 + g and 12 + g, the row's at each of four steps:
+// 4 x 4 bytes change places across the lanes that are 32 and 16 apart.
+__device__ inline uint32_t by_step(uint32_t w, int g) {
+  auto p = __builtin_amdgcn_permlane32_swap(w, w, false, false);      // of lanes 0 .. 31, and of lanes 32 .. 63
+  w = __builtin_amdgcn_perm(p[1], p[0], g & 2 ? 0x07060302u : 0x05040100u);
+  p = __builtin_amdgcn_permlane16_swap(w, w, false, false);           // of rows 0 and 2 of 16 lanes, and of 1 and 3
+  return __builtin_amdgcn_perm(p[1], p[0], g & 1 ? 0x07030501u : 0x06020400u);
+}
+
+template <int FA, int FB>
+__global__ __launch_bounds__(512) void k_mm_large(MatmulArgs a, uint32_t down, uint32_t across) {
+  typedef LargeShape<FA, FB> S;
+  extern __shared__ __align__(1024) uint8_t lds[];
+  constexpr int MT = S::TILE / S::WM / 16, NT = S::TILE / S::WN / 16, RA = S::RA, RB = S::RB, AHEAD = S::STAGES - 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int wm = wave / S::WN * (S::TILE / S::WM), wn = wave % S::WN * (S::TILE / S::WN);
+  int64_t m0, n0;
+  tile_at(down, across, m0, n0);
+  m0 *= S::TILE;
+  n0 *= S::TILE;
+  const int32_t blocks = (int32_t)a.blocks, steps = (blocks + 3) / 4;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+
+  typedef Loader<FA, S::TILE, S::STEP, S::WAVES> LoadA;
+  typedef Loader<FB, S::TILE, S::STEP, S::WAVES> LoadB;
+  constexpr int LOADS = LoadA::TURNS + LoadB::TURNS;
+  LoadA la;
+  LoadB lb;
+  la.init(a.a, m0, 0, blocks);
+  lb.init(a.b, n0, 0, blocks);
+  uint32_t slot = 0;   // where the next step goes
+  int32_t left = blocks;
+  auto done = [&] {
+    la.next();
+    lb.next();
+    left -= 4;
+    slot = slot + S::STAGE == S::STAGES * S::STAGE ? 0 : slot + S::STAGE;
+  };
+  auto load = [&] {
+#pragma unroll
+    for (int i = 0; i < LoadA::TURNS; ++i) la.load(base + slot, left * code_bytes(FA), i);
+#pragma unroll
+    for (int i = 0; i < LoadB::TURNS; ++i) lb.load(base + slot + S::A_BYTES, left * code_bytes(FB), i);
+    done();
+  };
+  // Scales of a chunk: waves 0 to 3 those of A, 64 rows each, the others B's.  Bytes behind the row's last block may be there too and are not looked at.
+  const uint32_t uwave = (uint32_t)__builtin_amdgcn_readfirstlane(wave);
+  const bool of_a = uwave < 4;
+  const Operand& so = of_a ? a.a : a.b;
+  const int64_t srow0 = of_a ? m0 : n0, srows = so.rows - srow0 < S::TILE ? so.rows - srow0 : S::TILE;
+  uint64_t scales_at = (uint64_t)(uintptr_t)(so.scales + srow0 * so.scale_ld);
+  int32_t scales_left = (int32_t)((srows - 1) * so.scale_ld + (blocks + 15) / 16 * 16), chunk_slot = 0;
+  const uint32_t scale_offset = ((uwave & 3) * 64 + lane) * (uint32_t)so.scale_ld;
+  auto load_scales = [&] {
+    const uint64_t from = scalar(scales_at);
+    const uint32_t size = (uint32_t)__builtin_amdgcn_readfirstlane(scales_left > 0 ? scales_left : 0);
+    to_lds(u32x4{(uint32_t)from, (uint32_t)(from >> 32), size, 0x00020000u}, scale_offset, base + S::STAGES * S::STAGE + chunk_slot + uwave * 1024u);
+    scales_at += 16;
+    scales_left -= 16;
+    chunk_slot ^= S::SCALES;
+  };
+
+  // where this lane's pieces are in a stage, and its words of scales: rows 16 apart are alike
+  int at_a[2], at_b[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    at_a[h] = (wm + r) * RA + swapped<RA>(r, FA == NT_MX_E2M1 ? g : 4 * h + g) * 16;
+    at_b[h] = S::A_BYTES + (wn + r) * RB + swapped<RB>(r, FB == NT_MX_E2M1 ? g : 4 * h + g) * 16;
+  }
+  const uint8_t* const scales_a = lds + S::STAGES * S::STAGE + 16 * (wm + r) + 4 * g;
+  const uint8_t* const scales_b = lds + S::STAGES * S::STAGE + 16 * (S::TILE + wn + r) + 4 * g;
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  load_scales();
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load();
+  landed_but<(AHEAD - 1) * LOADS>();
+
+  uint32_t here = 0, sa[MT], sb[NT];
+  for (int at = 0; at < steps; ++at) {
+    const uint8_t* const stage = lds + here;
+    if (at % S::STEPS == 0) {
+      // bytes behind the last block may be any, and NaN
+      const int32_t there = blocks - 4 * at - 4 * g;
+      const uint32_t mask = there >= 4 ? 0xffffffffu : there > 0 ? (1u << (8 * there)) - 1 : 0u;
+      const int chunk = (at / S::STEPS & 1) * S::SCALES;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sb[j] = by_step(*(const uint32_t*)(scales_b + chunk + 256 * j) & mask, g);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sa[i] = by_step(*(const uint32_t*)(scales_a + chunk + 256 * i) & mask, g);
+      load_scales();   // of the next chunk: beyond the descriptor behind the last one
+    }
+    // The step's loads go one by one between the products: all at once they keep the wave from reading and multiplying until they are
+    // accepted.  Not where the very next step needs them (8 bits both).
+    if (AHEAD == 1) load();
+    Frag<FA> fa[MT];
+    Frag<FB> fb[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      fb[j].w[0] = *(const u32x4*)(stage + at_b[0] + 16 * j * RB);
+      if (FB == NT_MX_E4M3) fb[j].w[FB == NT_MX_E4M3] = *(const u32x4*)(stage + at_b[1] + 16 * j * RB);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      fa[i].w[0] = *(const u32x4*)(stage + at_a[0] + 16 * i * RA);
+      if (FA == NT_MX_E4M3) fa[i].w[FA == NT_MX_E4M3] = *(const u32x4*)(stage + at_a[1] + 16 * i * RA);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = multiply<FA, FB, 0>(fb[j], sb[j], fa[i], sa[i], acc[i][j]);
+      if (AHEAD > 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (i < LoadA::TURNS)
+          la.load(base + slot, left * code_bytes(FA), i);
+        else if (i < LOADS)
+          lb.load(base + slot + S::A_BYTES, left * code_bytes(FB), i - LoadA::TURNS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (AHEAD > 1) done();
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[i] >>= 8;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sb[j] >>= 8;
+    here = here + S::STAGE == S::STAGES * S::STAGE ? 0 : here + S::STAGE;
+    landed_but<(AHEAD - 1) * LOADS>();
+  }
+  landed_but<0>();   // what was asked for behind the last step has gone to LDS too
+
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + wm + 16 * i + r;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int64_t col = n0 + wn + 16 * j + 4 * g, over = a.b.rows - col;
+      if (m < a.a.rows && over > 0) put4(a, m, col, acc[i][j], over < 4 ? (int)over : 4);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
@@ -489,7 +654,9 @@ struct MatmulPlan {
   uint32_t down, across; // tiles
   int splits, chunks;    // parts of the columns, and chunks of 512 in each
 };
-MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, int64_t ld) {
+// rows of scales at multiples of 16 bytes, within the reach of 32-bit offsets
+bool aligned16(const nt_mx& m) { return (((uintptr_t)m.scales | (uintptr_t)m.scale_ld) & 15) == 0 && m.scale_ld <= NT_MM_TILE_LD; }
+MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, int64_t ld, bool aligned) {
   MatmulPlan p;
   p.wide = dtype == NT_F32 && (fa == NT_MX_E4M3 || fb == NT_MX_E4M3);
   const int64_t chunks = ceil_div(K, NT_MM_CHUNK);
@@ -504,7 +671,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
     if (z > turns) z = turns;
     p.chunks = 0;
   } else {
-    p.kind = !p.wide && ceil_div(M, 256) * ceil_div(N, 256) >= 192 ? LARGE : MIDDLE;
+    p.kind = aligned && !p.wide && ceil_div(M, 256) * ceil_div(N, 256) >= 192 ? LARGE : MIDDLE;
     const int tile = p.kind == LARGE ? 256 : 128;
     p.down = (uint32_t)ceil_div(M, tile);
     p.across = (uint32_t)ceil_div(N, tile);
@@ -541,7 +708,7 @@ extern "C" {
 
 size_t normtest_mx_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, nt_mx_format a, nt_mx_format b, nt_dtype dtype) {
   if (M <= 0 || N <= 0 || K <= 0) return 0;
-  const MatmulPlan p = plan_of(M, N, K, a, b, dtype, 0);
+  const MatmulPlan p = plan_of(M, N, K, a, b, dtype, 0, true);
   return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
 
@@ -564,7 +731,7 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
     hipLaunchKernelGGL(k_mm_empty, dim3(grid_of(M * N)), dim3(256), 0, st, args);
     return hip_code(hipGetLastError());
   }
-  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype, a->ld > b->ld ? a->ld : b->ld);
+  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype, a->ld > b->ld ? a->ld : b->ld, aligned16(*a) && aligned16(*b));
   if (p.splits > 1) {
     if (!workspace || workspace_bytes < (size_t)p.splits * (size_t)M * (size_t)N * sizeof(float)) return NT_ERR_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace & 15) return NT_ERR_BAD_ARG;
@@ -586,7 +753,10 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
         if (p.wide) return p.rows == 1 ? thin(k_mm_thin<A, B, W, 1>) : thin(k_mm_thin<A, B, W, 2>);
         return p.rows == 1 ? thin(k_mm_thin<A, B, false, 1>) : thin(k_mm_thin<A, B, false, 2>);
       }
-      if (p.kind == LARGE) return tile(k_mm_tile<A, B, false, 256, 256, NT_MM_LM, NT_MM_LN>, 64 * NT_MM_LM * NT_MM_LN, TileShape<A, B, false, 256, 256, NT_MM_LM, NT_MM_LN>::LDS);
+      if (p.kind == LARGE) {
+        hipLaunchKernelGGL((k_mm_large<A, B>), dim3(p.down * p.across), dim3(512), (LargeShape<A, B>::LDS), st, args, p.down, p.across);
+        return hip_code(hipGetLastError());
+      }
       if (p.wide) return tile(k_mm_tile<A, B, W, 128, 128, 2, 2>, 256, TileShape<A, B, W, 128, 128, 2, 2>::LDS);
       return tile(k_mm_tile<A, B, false, 128, 128, 2, 2>, 256, TileShape<A, B, false, 128, 128, 2, 2>::LDS);
     });

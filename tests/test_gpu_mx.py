@@ -128,10 +128,12 @@ def test_dequantize(form, dtype):
 
 # ---- product -------------------------------------------------------------------------------
 
-def operand(rows, cols, form, seed, pad=0, spread=0):
-    """A microscaled matrix of random codes and scales, whose rows are `pad` blocks longer than they need."""
+def operand(rows, cols, form, seed, pad=0, spread=0, aligned=False):
+    """A microscaled matrix of random codes and scales, whose rows are `pad` blocks longer than they need, or begin at multiples of 16 scales."""
     gen = torch.Generator().manual_seed(seed)
     blocks = -(-cols // 32)
+    if aligned:
+        pad = -blocks % 16 + 16 * pad
     per = R.BYTES[FORMS[form]]
     if form == "e2m1":
         codes = torch.randint(256, (rows, (blocks + pad) * per), dtype=torch.uint8, generator=gen)
@@ -228,8 +230,8 @@ def test_product_scales(form, form_b):
 def test_product_of_many_tiles(form, form_b):
     """More tiles than the chip takes at once, edges that end inside one, and sums over parts of the columns: against a product in 64 bits on the GPU."""
     for M, N, K, dtype in ((1000, 2100, 300, "bf16"), (700, 900, 5000, "f32"), (64, 128, 40000, "f32"), (2, 40, 70000, "bf16"), (520, 1030, 1500, "f16"),
-                           (3700, 3700, 700, "bf16")):
-        a, b = operand(M, K, form, M), operand(N, K, form_b, N)
+                           (3700, 3700, 700, "bf16"), (3333, 4000, 2100, "f16"), (4100, 3601, 31, "bf16")):
+        a, b = operand(M, K, form, M, aligned=M > 3000), operand(N, K, form_b, N, pad=1, aligned=N > 3000)
         na, nb = torch.from_numpy(R.numbers(a)).to(DEV), torch.from_numpy(R.numbers(b)).to(DEV)
         want = na @ nb.t().contiguous()
         got = B.normtest_mx_matmul(a, b, dtype=TYPES[dtype]).double()
