@@ -264,9 +264,10 @@ __device__ inline int swapped(int row, int piece) {
 }
 
 // 16 bytes a lane from memory to consecutive bytes of LDS.  What lies beyond the descriptor's size reads as zeros.  The compiler does not know
-// of these loads: whoever reads the LDS waits for them by landed().
+// of these loads: whoever reads the LDS waits for them by landed().  Nor does it see that the descriptor is read here: a vector instruction (reading
+// the first lane) that has just written one of its registers needs five wait states before, or an old value is used.
 __device__ inline void to_lds(u32x4 from, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(from), "s"(to) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(from), "s"(to) : "memory", "m0");
 }
 // all loads of this wave have arrived, all its LDS accesses are done, and every other wave of the block is here too
 __device__ inline void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
@@ -676,7 +677,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
     p.down = (uint32_t)ceil_div(M, tile);
     p.across = (uint32_t)ceil_div(N, tile);
     const int64_t tiles = (int64_t)p.across * p.down;
-    if (tiles < 256) z = 512 / tiles;
+    if (p.kind == MIDDLE && tiles < 256) z = 512 / tiles;
     if (z > chunks / 2) z = chunks / 2;
     if (z < 1) z = 1;
     p.chunks = (int)ceil_div(chunks, z);
