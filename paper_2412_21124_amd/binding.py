@@ -215,7 +215,8 @@ def lib(path: Optional[str] = None):
         L.normtest_strerror.restype = ctypes.c_char_p
         for name in ("normtest_step", "normtest_step_rows", "normtest_step_clipped", "normtest_adamw_gbar", "normtest_layer_stats",
                      "normtest_workspace_bytes_for", "normtest_grad_norm", "normtest_clip_grads", "normtest_accumulate",
-                     "normtest_adamw_tensors"):
+                     "normtest_adamw_tensors", "normtest_mx_quantize", "normtest_mx_dequantize", "normtest_mx_matmul", "normtest_rms_norm",
+                     "normtest_rms_norm_backward"):
             setattr(L, name + "_entry", ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
         if _lib is None:
             _fast = _load_callpath()
@@ -875,16 +876,26 @@ class MxTensor:
         ld = codes.stride(0) if self.rows > 1 else blocks * _MX_BLOCK_BYTES[format]
         if self.rows > 0 and cols > 0 and (codes.data_ptr() % 16 or ld % 16):
             raise ValueError("rows of codes must begin at multiples of 16 bytes")
-        self._record = nt_mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols, ld, scales.stride(0) if self.rows > 1 else blocks, format, 0)
+        scale_ld = scales.stride(0) if self.rows > 1 else blocks
+        self._record = nt_mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols, ld, scale_ld, format, 0)
+        self._made_of = _place(codes), _place(scales)
+        lib()
+        self.native = _fast and _fast.make_mx(codes, scales, self.rows, cols, ld, scale_ld, format) or None   # as the native call path knows it
 
     @property
     def shape(self):
         return (self.rows, self.cols)
 
     def pointer(self):
-        """The library's record of this matrix, as it is now."""
-        self._record.codes, self._record.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        """The library's record of this matrix."""
+        if (_place(self.codes), _place(self.scales)) != self._made_of:
+            raise RuntimeError("codes or scales of a microscaled matrix have other memory or another shape than when it was made")
         return ctypes.byref(self._record)
+
+
+def _native_mx(m):
+    """What the native call path knows a matrix by: None for none, False for what it does not take."""
+    return None if m is None else (m.native or False) if type(m) is MxTensor else False
 
 
 def make_mx(rows: int, cols: int, format: int = NT_MX_E2M1, device=None) -> MxTensor:
@@ -952,6 +963,8 @@ def normtest_mx_quantize(src: torch.Tensor, out: Optional[MxTensor] = None, out_
     448), or with `fit` the least that clamps nothing.  noise: uint8, src's shape; a random byte for every element rounds it up with the
     probability of its fraction instead of to nearest even.  A block with a NaN or an infinity reads as NaN."""
     where = "normtest_mx_quantize"
+    if stream is None and _fast and _done(_fast.mx_quantize(_lib.normtest_mx_quantize_entry, src, _native_mx(out), _native_mx(out_t), fit, noise), where):
+        return
     address, dtype, ld = _numbers(where, "src", src)
     (rows, cols), dev = src.shape, src.device
     if out is None and out_t is None:
@@ -970,6 +983,8 @@ def normtest_mx_dequantize(src: MxTensor, out: Optional[torch.Tensor] = None, *,
                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The numbers that src stands for, into out (any of the three types) or a new matrix of `dtype`."""
     where = "normtest_mx_dequantize"
+    if stream is None and out is not None and _fast and _done(_fast.mx_dequantize(_lib.normtest_mx_dequantize_entry, _native_mx(src), out), where):
+        return out
     record = _mx(where, "src", src)
     if out is None:
         out = _fresh(src.shape, dtype, src.device, stream)
@@ -1002,6 +1017,9 @@ def normtest_mx_matmul(a: MxTensor, b: MxTensor, out: Optional[torch.Tensor] = N
     A weight's gradient with beta = 1 and a row of the norm test as out is accumulated there.  workspace: device memory of
     normtest_mx_matmul_workspace_bytes(a, b, out.dtype) bytes; made here if it is not given."""
     where = "normtest_mx_matmul"
+    if stream is None and out is not None and _fast:
+        if _done(_fast.mx_matmul(_lib.normtest_mx_matmul_entry, _native_mx(a), _native_mx(b), out, scale, beta, workspace), where):
+            return out
     pa, pb = _mx(where, "a", a), _mx(where, "b", b)
     dev = a.device
     if b.device != dev or a.cols != b.cols:
@@ -1027,6 +1045,9 @@ def normtest_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], out: Opti
     """h = x + residual (stored to sum_out in x's type), rstd = 1 / sqrt(mean(h^2) + eps) per row (float32), and h rstd weight into out (x's
     type), out_mx (codes and scales, `fit` as in normtest_mx_quantize) or both.  Everything but x may be left out; sum_out may be x or residual."""
     where = "normtest_rms_norm"
+    if stream is None and _fast:
+        if _done(_fast.rms_norm(_lib.normtest_rms_norm_entry, x, weight, out, residual, eps, sum_out, _native_mx(out_mx), rstd, fit), where):
+            return
     px, kind, x_ld = _numbers(where, "x", x)
     (rows, cols), dev = x.shape, x.device
     pr, _, r_ld = (None, 0, 0) if residual is None else _numbers(where, "residual", residual, x.shape, x.dtype, dev)
@@ -1051,6 +1072,9 @@ def normtest_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Option
     dsum (what else comes back to h) included, and dweight <- beta dweight + scale (its gradient), float32.  dx may be dy or dsum.
     workspace: device memory of normtest_rms_norm_workspace_bytes(rows, cols) bytes for dweight; made here if it is not given."""
     where = "normtest_rms_norm_backward"
+    if stream is None and _fast:
+        if _done(_fast.rms_norm_backward(_lib.normtest_rms_norm_backward_entry, dy, h, weight, rstd, dx, dsum, dweight, scale, beta, workspace), where):
+            return
     py, kind, y_ld = _numbers(where, "dy", dy)
     (rows, cols), dev = dy.shape, dy.device
     ph, _, h_ld = _numbers(where, "h", h, dy.shape, dy.dtype, dev)

@@ -415,6 +415,185 @@ PyObject* adamw_tensors(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- microscaled matrices and the norm ----
+// A microscaled matrix as the binding made it: its bytes, where they were then, and the library's record.
+struct Mx {
+  at::Tensor codes, scales;
+  nt_mx record;
+  c10::Device device = c10::Device(c10::DeviceType::CPU);
+};
+const char mx_name[] = "normtest.mx";
+void mx_free(PyObject* capsule) { delete (Mx*)PyCapsule_GetPointer(capsule, mx_name); }
+// make_mx(codes, scales, rows, cols, ld, scale_ld, format)
+PyObject* make_mx(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    std::unique_ptr<Mx> m(new Mx());
+    m->codes = tensor(a[0]);
+    m->scales = tensor(a[1]);
+    m->device = m->codes.device();
+    m->record = {m->codes.data_ptr(), m->scales.data_ptr(), integer(a[2]), integer(a[3]), integer(a[4]), integer(a[5]), small(a[6]), 0};
+    PyObject* capsule = PyCapsule_New(m.get(), mx_name, mx_free);
+    if (!capsule) throw Refused();
+    m.release();
+    return capsule;
+  });
+}
+// The matrix behind a capsule, its bytes where they were, rows x cols (negative: any) on this device.
+const nt_mx* mx_of(PyObject* o, const c10::Device& device, int64_t rows, int64_t cols) {
+  if (!PyCapsule_IsValid(o, mx_name)) throw Refused();
+  const Mx& m = *(const Mx*)PyCapsule_GetPointer(o, mx_name);
+  if (m.device != device || m.codes.data_ptr() != m.record.codes || m.scales.data_ptr() != m.record.scales || m.codes.size(0) != m.record.rows ||
+      m.scales.size(0) != m.record.rows || (rows >= 0 && (m.record.rows != rows || m.record.cols != cols)))
+    throw Refused();
+  return &m.record;
+}
+const c10::Device& device_of_mx(PyObject* o) {
+  if (!PyCapsule_IsValid(o, mx_name)) throw Refused();
+  const Mx& m = *(const Mx*)PyCapsule_GetPointer(o, mx_name);
+  if (c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != m.device) throw Refused();
+  return m.device;
+}
+// A matrix of numbers: two dimensions, the last one dense.
+struct Numbers {
+  void* data;
+  int64_t rows, cols, ld;
+  nt_dtype dtype;
+};
+Numbers numbers_of(PyObject* o, const c10::Device* device, const Numbers* like, bool any_type) {
+  const at::Tensor& t = tensor(o);
+  if (device ? t.device() != *device : !t.is_cuda()) throw Refused();
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) throw Refused();
+  const auto kind = t.scalar_type();
+  if (kind != at::kFloat && kind != at::kBFloat16 && kind != at::kHalf) throw Refused();
+  Numbers m = {t.data_ptr(), t.size(0), t.size(1), t.size(0) > 1 ? t.stride(0) : t.size(1), kind == at::kFloat ? NT_F32 : kind == at::kBFloat16 ? NT_BF16 : NT_F16};
+  if (like && (m.rows != like->rows || m.cols != like->cols || (!any_type && m.dtype != like->dtype))) throw Refused();
+  return m;
+}
+Numbers numbers_or_none(PyObject* o, const c10::Device& device, const Numbers& like) {
+  return o == Py_None ? Numbers{nullptr, 0, 0, 0, like.dtype} : numbers_of(o, &device, &like, false);
+}
+float* floats_of(PyObject* o, const c10::Device& device, int64_t count, bool required) {
+  if (o == Py_None && !required) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != at::kFloat || t.device() != device || !t.is_contiguous() || t.numel() != count) throw Refused();
+  return (float*)t.data_ptr();
+}
+Bytes scratch_of(PyObject* o, const c10::Device& device) {
+  if (o == Py_None) return {nullptr, 0};
+  const at::Tensor& t = tensor(o);
+  if (t.device() != device || !t.is_contiguous()) throw Refused();
+  return {t.data_ptr(), (size_t)(t.numel() * t.element_size())};
+}
+bool truth(PyObject* o) {
+  if (o != Py_True && o != Py_False) throw Refused();
+  return o == Py_True;
+}
+// As enqueue; a call that wants scratch memory and was given none is made again by Python, which allocates it.
+template <class CALL>
+PyObject* enqueue_with(const Bytes& scratch, CALL call) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call();
+  Py_END_ALLOW_THREADS
+  if (rc == NT_ERR_WORKSPACE_TOO_SMALL && !scratch.data) throw Refused();
+  return PyLong_FromLong(rc);
+}
+
+// mx_quantize(entry, src, out, out_t, fit, noise)
+PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&] {
+    auto* f = entry<decltype(normtest_mx_quantize)>(a[0]);
+    const Numbers src = numbers_of(a[1], nullptr, nullptr, false);
+    const c10::Device device = tensor(a[1]).device();
+    check_device(tensor(a[1]));
+    const nt_mx* out = a[2] == Py_None ? nullptr : mx_of(a[2], device, src.rows, src.cols);
+    const nt_mx* out_t = a[3] == Py_None ? nullptr : mx_of(a[3], device, src.cols, src.rows);
+    if (!out && !out_t) throw Refused();
+    const uint32_t flags = truth(a[4]) ? NT_MX_FIT : 0u;
+    const uint8_t* noise = nullptr;
+    int64_t noise_ld = 0;
+    if (a[5] != Py_None) {
+      const at::Tensor& t = tensor(a[5]);
+      if (t.scalar_type() != at::kByte || t.device() != device || t.dim() != 2 || t.size(0) != src.rows || t.size(1) != src.cols ||
+          (src.cols > 1 && t.stride(1) != 1))
+        throw Refused();
+      noise = (const uint8_t*)t.data_ptr();
+      noise_ld = src.rows > 1 ? t.stride(0) : src.cols;
+    }
+    void* st = stream_of(device);
+    return enqueue([&] { return f(src.data, src.dtype, src.rows, src.cols, src.ld, noise, noise_ld, out, out_t, flags, st); });
+  });
+}
+
+// mx_dequantize(entry, src, out)
+PyObject* mx_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 3, [&] {
+    auto* f = entry<decltype(normtest_mx_dequantize)>(a[0]);
+    const c10::Device& device = device_of_mx(a[1]);
+    const Numbers out = numbers_of(a[2], &device, nullptr, false);
+    const nt_mx* src = mx_of(a[1], device, out.rows, out.cols);
+    void* st = stream_of(device);
+    return enqueue([&] { return f(src, out.data, out.dtype, out.ld, st); });
+  });
+}
+
+// mx_matmul(entry, a, b, out, scale, beta, workspace)
+PyObject* mx_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&] {
+    auto* f = entry<decltype(normtest_mx_matmul)>(a[0]);
+    const c10::Device& device = device_of_mx(a[1]);
+    const nt_mx *x = mx_of(a[1], device, -1, -1), *y = mx_of(a[2], device, -1, -1);
+    const Numbers out = numbers_of(a[3], &device, nullptr, false);
+    if (x->cols != y->cols || out.rows != x->rows || out.cols != y->rows) throw Refused();
+    const double scale = number(a[4]), beta = number(a[5]);
+    const Bytes ws = scratch_of(a[6], device);
+    void* st = stream_of(device);
+    return enqueue_with(ws, [&] { return f(x, y, scale, beta, out.data, out.dtype, out.ld, ws.data, ws.size, st); });
+  });
+}
+
+// rms_norm(entry, x, weight, out, residual, eps, sum_out, out_mx, rstd, fit)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    auto* f = entry<decltype(normtest_rms_norm)>(a[0]);
+    const Numbers x = numbers_of(a[1], nullptr, nullptr, false);
+    const c10::Device device = tensor(a[1]).device();
+    check_device(tensor(a[1]));
+    const float* weight = floats_of(a[2], device, x.cols, false);
+    const Numbers out = numbers_or_none(a[3], device, x), residual = numbers_or_none(a[4], device, x), sum = numbers_or_none(a[6], device, x);
+    const double eps = number(a[5]);
+    const nt_mx* mx = a[7] == Py_None ? nullptr : mx_of(a[7], device, x.rows, x.cols);
+    float* rstd = floats_of(a[8], device, x.rows, false);
+    const uint32_t flags = truth(a[9]) ? NT_MX_FIT : 0u;
+    void* st = stream_of(device);
+    return enqueue([&] {
+      return f(x.data, x.ld, residual.data, residual.ld, weight, eps, x.dtype, x.rows, x.cols, sum.data, sum.ld, out.data, out.ld, mx, rstd, flags, st);
+    });
+  });
+}
+
+// rms_norm_backward(entry, dy, h, weight, rstd, dx, dsum, dweight, scale, beta, workspace)
+PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&] {
+    auto* f = entry<decltype(normtest_rms_norm_backward)>(a[0]);
+    const Numbers dy = numbers_of(a[1], nullptr, nullptr, false);
+    const c10::Device device = tensor(a[1]).device();
+    check_device(tensor(a[1]));
+    const Numbers h = numbers_of(a[2], &device, &dy, false);
+    const float *weight = floats_of(a[3], device, dy.cols, false), *rstd = floats_of(a[4], device, dy.rows, true);
+    const Numbers dx = numbers_or_none(a[5], device, dy), dsum = numbers_or_none(a[6], device, dy);
+    float* dweight = floats_of(a[7], device, dy.cols, false);
+    if (a[5] == Py_None && a[7] == Py_None) throw Refused();
+    const double scale = number(a[8]), beta = number(a[9]);
+    const Bytes ws = scratch_of(a[10], device);
+    void* st = stream_of(device);
+    return enqueue_with(ws, [&] {
+      return f(dy.data, dy.ld, h.data, h.ld, weight, rstd, dsum.data, dsum.ld, dy.dtype, dy.rows, dy.cols, dx.data, dx.ld, dweight, scale, beta,
+               ws.data, ws.size, st);
+    });
+  });
+}
+
 // init(nt_hyper, nt_shard_info, torch.nn.Parameter, torch._C._cuda_getCurrentRawStream)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 4, [&]() -> PyObject* {
@@ -430,7 +609,8 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init),       FAST(step),        FAST(step_clipped), FAST(step_rows),
                          FAST(adamw_gbar), FAST(layer_stats), FAST(make_list), FAST(unchanged), FAST(grad_norm), FAST(clip_grads), FAST(accumulate),
-                         FAST(adamw_tensors), {nullptr, nullptr, 0, nullptr}};
+                         FAST(adamw_tensors), FAST(make_mx), FAST(mx_quantize), FAST(mx_dequantize), FAST(mx_matmul), FAST(rms_norm),
+                         FAST(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_callpath", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
