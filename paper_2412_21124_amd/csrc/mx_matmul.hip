@@ -14,6 +14,11 @@
 #define NT_MM_CHUNK 512            // columns that a wave takes at a time: 16 blocks, four for a lane
 #define NT_MM_CHUNK_BLOCKS 16
 #define NT_MM_THIN_WAVES 4
+// Up to 32 rows always, and up to 64 where 128 x 128 tiles are too few (64 x 2048 x 2048 11.6 -> 7.4 us; 64 x 16384 x 4096, 128 tiles, 19.7 -> 25.3).
+#define NT_MM_THIN_ROWS 32
+#define NT_MM_THIN_MORE_ROWS 64
+#define NT_MM_THIN_TILES 96
+#define NT_MM_THIN_MANY 512        // blocks from which a wave takes 32 columns and not 16 (24 x 50257 x 768 16.4 -> 13.5 us, 1 x 16384 x 4096 8.8 -> 8.2)
 #define NT_MM_TILE_LD (1ll << 22)   // bytes from row to row that 32-bit offsets into a tile allow
 
 namespace {
@@ -92,15 +97,20 @@ __device__ inline void put4(const MatmulArgs& a, int64_t m, int64_t col, f32x4 x
     }
 }
 
-__global__ __launch_bounds__(256) void k_mm_join(MatmulArgs a, int splits) {
-  const int64_t n = a.a.rows * a.b.rows;
+// The parts' sum, in order, four columns of a row to a thread.
+__global__ __launch_bounds__(256) void k_mm_join(MatmulArgs a, int splits, uint32_t quads) {
+  const int64_t n = a.a.rows * a.b.rows, all = a.a.rows * quads;
   const float* const parts = a.parts;
   a.parts = nullptr;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = all < 1ll << 32 ? (uint32_t)i / quads : i / quads, col = 4 * (i - m * quads), left = a.b.rows - col;
+    const float* p = parts + m * a.b.rows + col;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) x[0] += parts[s * n + i];
-    const int64_t m = i / a.b.rows;
-    put4(a, m, i - m * a.b.rows, x, 1);
+    for (int s = 0; s < splits; ++s, p += n) {
+      const Raw<NT_F32> r = left >= 4 ? Raw<NT_F32>{{*(const u32x4_word*)p, {}}} : load_part<NT_F32>(p, (int)left);
+      x += __builtin_bit_cast(f32x4, r.w[0]);
+    }
+    put4(a, m, col, x, left < 4 ? (int)left : 4);
   }
 }
 
@@ -143,12 +153,22 @@ __device__ inline f32x4 multiply(const Frag<FB>& b, uint32_t sb, const Frag<FA>&
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(registers(b), registers(a), c, CODE_B, CODE_A, BYTE, (int)sb, BYTE, (int)sa);
 }
 
+// Lane (r, g) has the scales of blocks 4 g .. 4 g + 3 of a row, and gets those of the blocks g, 4 + g, 8 + g and 12 + g, the row's at each of four steps:
+// 4 x 4 bytes change places across the lanes that are 32 and 16 apart.
+__device__ inline uint32_t by_step(uint32_t w, int g) {
+  auto p = __builtin_amdgcn_permlane32_swap(w, w, false, false);      // of lanes 0 .. 31, and of lanes 32 .. 63
+  w = __builtin_amdgcn_perm(p[1], p[0], g & 2 ? 0x07060302u : 0x05040100u);
+  p = __builtin_amdgcn_permlane16_swap(w, w, false, false);           // of rows 0 and 2 of 16 lanes, and of 1 and 3
+  return __builtin_amdgcn_perm(p[1], p[0], g & 1 ? 0x07030501u : 0x06020400u);
+}
+
 // ---------------------------------------------------------------------------------------------
 // Few rows
 // ---------------------------------------------------------------------------------------------
-// A wave takes 16 columns of the result and MT x 16 rows, straight from memory to registers; the waves of a block (and blockIdx.z) take every
-// 4th (4 gridDim.z-th) chunk of 512 columns of A and B, and are joined through LDS.  Lane (r, g) has of a chunk the blocks 4 g .. 4 g + 3 of row r, 64
-// consecutive bytes in 4 bits, and one word of scales.
+// A wave takes NT x 16 columns of the result and MT x 16 rows, straight from memory to registers, a chunk of 512 columns of A and B at a time.  `along` of
+// a block's four waves (and blockIdx.z) share out the chunks, and are joined through LDS; the others have columns of their own.  Lanes that hold pieces
+// of one row load 64 bytes of it side by side, and one word of scales each, which then change places.  (Four blocks of a lane side by
+// side need no change, but every lane loads from a cache line of its own: 24 x 50257 x 768 19.7 us.)
 template <int F, bool WIDE>
 struct Chunk {
   Frag<F> f[4];
@@ -157,7 +177,6 @@ struct Chunk {
     const int g = (threadIdx.x & 63) / 16;
     const bool there = row < o.rows;
     const uint8_t* const codes = o.codes + row * o.ld;
-    const int64_t b0 = block0 + 4 * g;
     auto piece = [&](int64_t block, int half) {
       u32x4 x = {0u, 0u, 0u, 0u};
       if (there && (whole || block < blocks)) x = *(const u32x4*)(codes + block * code_bytes(F) + 16 * half);
@@ -165,80 +184,96 @@ struct Chunk {
     };
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
+      const int64_t first = block0 + 4 * u;
       if (F == NT_MX_E2M1) {
-        f[u].w[0] = piece(b0 + u, 0);
+        f[u].w[0] = piece(first + g, 0);
       } else if (WIDE) {
-        f[u].w[0] = piece(b0 + u, 0);
-        f[u].w[F == NT_MX_E4M3] = piece(b0 + u, 1);
+        f[u].w[0] = piece(first + g, 0);
+        f[u].w[F == NT_MX_E4M3] = piece(first + g, 1);
       } else {   // elements 16 g .. of the instruction's first and second 64
-        f[u].w[0] = piece(block0 + 4 * (g / 2) + u, g & 1);
-        f[u].w[F == NT_MX_E4M3] = piece(block0 + 4 * (2 + g / 2) + u, g & 1);
+        f[u].w[0] = piece(first + g / 2, g & 1);
+        f[u].w[F == NT_MX_E4M3] = piece(first + 2 + g / 2, g & 1);
       }
     }
-    scales = 0;
+    uint32_t word = 0;
+    const int64_t b0 = block0 + 4 * g;
     if (there) {
       const uint8_t* const s = o.scales + row * o.scale_ld;
       if (whole || b0 + 4 <= blocks) {
-        scales = *(const u32_any*)(s + b0);
+        word = *(const u32_any*)(s + b0);
       } else {
         for (int u = 0; u < 3; ++u)
-          if (b0 + u < blocks) scales |= (uint32_t)s[b0 + u] << (8 * u);
+          if (b0 + u < blocks) word |= (uint32_t)s[b0 + u] << (8 * u);
       }
     }
+    scales = word;
   }
+  // where the scales are needed: what the lane loaded is its neighbours'
+  __device__ inline void settle() { scales = by_step(scales, (threadIdx.x & 63) / 16); }
 };
 
-template <int FA, int FB, bool WIDE, int MT>
-__global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a) {
-  __shared__ f32x4 sums[NT_MM_THIN_WAVES][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
-  f32x4 acc[MT];
+template <int FA, int FB, bool WIDE, int MT, int NT>
+__global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a, int along) {
+  __shared__ f32x4 sums[NT_MM_THIN_WAVES][MT * NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, part = wave % along;
+  const int64_t n0 = ((int64_t)blockIdx.x * (NT_MM_THIN_WAVES / along) + wave / along) * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
+  f32x4 acc[MT][NT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int64_t chunks = (a.blocks + NT_MM_CHUNK_BLOCKS - 1) / NT_MM_CHUNK_BLOCKS;
-  for (int64_t c = (int64_t)blockIdx.z * NT_MM_THIN_WAVES + wave; c < chunks; c += (int64_t)gridDim.z * NT_MM_THIN_WAVES) {
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t chunks = (a.blocks + NT_MM_CHUNK_BLOCKS - 1) / NT_MM_CHUNK_BLOCKS, step = (int64_t)gridDim.z * along;
+  for (int64_t c = (int64_t)blockIdx.z * along + part; c < chunks; c += step) {
     const int64_t block0 = c * NT_MM_CHUNK_BLOCKS;
     const bool whole = block0 + NT_MM_CHUNK_BLOCKS <= a.blocks;
-    Chunk<FB, WIDE> b;
+    Chunk<FB, WIDE> b[NT];
     Chunk<FA, WIDE> x[MT];
-    b.load(a.b, n0 + r, block0, a.blocks, whole);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) b[n].load(a.b, n0 + 16 * n + r, block0, a.blocks, whole);
 #pragma unroll
     for (int t = 0; t < MT; ++t) x[t].load(a.a, m0 + 16 * t + r, block0, a.blocks, whole);
-    if (!WIDE) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        acc[t] = multiply<FA, FB, 0>(b.f[0], b.scales, x[t].f[0], x[t].scales, acc[t]);
-        acc[t] = multiply<FA, FB, 1>(b.f[1], b.scales, x[t].f[1], x[t].scales, acc[t]);
-        acc[t] = multiply<FA, FB, 2>(b.f[2], b.scales, x[t].f[2], x[t].scales, acc[t]);
-        acc[t] = multiply<FA, FB, 3>(b.f[3], b.scales, x[t].f[3], x[t].scales, acc[t]);
-      }
+    for (int n = 0; n < NT; ++n) b[n].settle();
+#pragma unroll
+    for (int t = 0; t < MT; ++t) x[t].settle();
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[t][n] = multiply<FA, FB, 0>(b[n].f[0], b[n].scales, x[t].f[0], x[t].scales, acc[t][n]);
+          acc[t][n] = multiply<FA, FB, 1>(b[n].f[1], b[n].scales, x[t].f[1], x[t].scales, acc[t][n]);
+          acc[t][n] = multiply<FA, FB, 2>(b[n].f[2], b[n].scales, x[t].f[2], x[t].scales, acc[t][n]);
+          acc[t][n] = multiply<FA, FB, 3>(b[n].f[3], b[n].scales, x[t].f[3], x[t].scales, acc[t][n]);
+        }
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float sb = grow((b.scales >> (8 * u)) & 255u);
-        float sa[MT];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) sa[t] = grow((x[t].scales >> (8 * u)) & 255u);
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const bf16x8 wb = widened<FB>(b.f[u], p, sb);
+          bf16x8 wb[NT];
 #pragma unroll
-          for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, widened<FA>(x[t].f[u], p, sa[t]), acc[t], 0, 0, 0);
+          for (int n = 0; n < NT; ++n) wb[n] = widened<FB>(b[n].f[u], p, grow((b[n].scales >> (8 * u)) & 255u));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            const bf16x8 wa = widened<FA>(x[t].f[u], p, grow((x[t].scales >> (8 * u)) & 255u));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[n], wa, acc[t][n], 0, 0, 0);
+          }
         }
-      }
     }
   }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sums[wave][t * NT + n][lane] = acc[t][n];
   __syncthreads();
   if (gridDim.z > 1) a.parts += (int64_t)blockIdx.z * a.a.rows * a.b.rows;
-  for (int t = wave; t < MT; t += NT_MM_THIN_WAVES) {
-    f32x4 x = sums[0][t][lane];
-#pragma unroll
-    for (int w = 1; w < NT_MM_THIN_WAVES; ++w) x += sums[w][t][lane];
-    const int64_t m = m0 + 16 * t + r, col = n0 + 4 * (lane / 16), left = a.b.rows - col;
-    if (m < a.a.rows && left > 0) put4(a, m, col, x, left < 4 ? (int)left : 4);
+  for (int i = part; i < MT * NT; i += along) {   // the waves that share columns write them, a 16 x 16 piece each
+    f32x4 y = sums[wave - part][i][lane];
+    for (int w = 1; w < along; ++w) y += sums[wave - part + w][i][lane];
+    const int64_t m = m0 + 16 * (i / NT) + r, col = n0 + 16 * (i % NT) + 4 * (lane / 16), left = a.b.rows - col;
+    if (m < a.a.rows && left > 0) put4(a, m, col, y, left < 4 ? (int)left : 4);
   }
 }
 
@@ -499,15 +534,6 @@ __device__ inline void landed_but() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
-// Lane (r, g) has the scales of blocks 4 g .. 4 g + 3 of a row, and gets those of the blocks g, 4 + g, 8 + g and 12 + g, the row's at each of four steps:
-// 4 x 4 bytes change places across the lanes that are 32 and 16 apart.
-__device__ inline uint32_t by_step(uint32_t w, int g) {
-  auto p = __builtin_amdgcn_permlane32_swap(w, w, false, false);      // of lanes 0 .. 31, and of lanes 32 .. 63
-  w = __builtin_amdgcn_perm(p[1], p[0], g & 2 ? 0x07060302u : 0x05040100u);
-  p = __builtin_amdgcn_permlane16_swap(w, w, false, false);           // of rows 0 and 2 of 16 lanes, and of 1 and 3
-  return __builtin_amdgcn_perm(p[1], p[0], g & 1 ? 0x07030501u : 0x06020400u);
-}
-
 template <int FA, int FB>
 __global__ __launch_bounds__(512) void k_mm_large(MatmulArgs a, uint32_t down, uint32_t across) {
   typedef LargeShape<FA, FB> S;
@@ -651,7 +677,7 @@ __global__ __launch_bounds__(512) void k_mm_large(MatmulArgs a, uint32_t down, u
 enum { THIN, MIDDLE, LARGE };
 struct MatmulPlan {
   bool wide;
-  int kind, rows;        // rows: THIN: 16-row groups of a wave
+  int kind, rows, cols, along;   // of THIN: 16-row and 16-column groups of a wave, and the block's waves that share chunks
   uint32_t down, across; // tiles
   int splits, chunks;    // parts of the columns, and chunks of 512 in each
 };
@@ -661,13 +687,17 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
   MatmulPlan p;
   p.wide = dtype == NT_F32 && (fa == NT_MX_E4M3 || fb == NT_MX_E4M3);
   const int64_t chunks = ceil_div(K, NT_MM_CHUNK);
-  p.rows = M <= 16 ? 1 : 2;
+  p.rows = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  p.along = chunks >= 4 ? 4 : chunks >= 2 ? 2 : 1;
+  p.cols = 1;
   int64_t z = 1;
-  if (M <= 32 || ld > NT_MM_TILE_LD) {
+  if (M <= NT_MM_THIN_ROWS || (M <= NT_MM_THIN_MORE_ROWS && ceil_div(N, 128) < NT_MM_THIN_TILES) || ld > NT_MM_TILE_LD) {
     p.kind = THIN;
-    p.across = (uint32_t)ceil_div(N, 16);
+    const int beside = NT_MM_THIN_WAVES / p.along;
     p.down = (uint32_t)ceil_div(M, 16 * p.rows);
-    const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(chunks, NT_MM_THIN_WAVES);
+    if (ceil_div(N, 32 * beside) * p.down >= NT_MM_THIN_MANY) p.cols = 2;
+    p.across = (uint32_t)ceil_div(N, 16 * p.cols * beside);
+    const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(chunks, p.along);
     if (tiles < 256) z = ceil_div(512, tiles);
     if (z > turns) z = turns;
     p.chunks = 0;
@@ -743,7 +773,7 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
       constexpr int A = decltype(fa)::value, B = decltype(fb)::value;
       constexpr bool W = A == NT_MX_E4M3 || B == NT_MX_E4M3;
       auto thin = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(p.across, p.down, (uint32_t)p.splits), dim3(64 * NT_MM_THIN_WAVES), 0, st, args);
+        hipLaunchKernelGGL(kernel, dim3(p.across, p.down, (uint32_t)p.splits), dim3(64 * NT_MM_THIN_WAVES), 0, st, args, p.along);
         return hip_code(hipGetLastError());
       };
       auto tile = [&](auto kernel, int threads, int lds) {
@@ -751,8 +781,16 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
         return hip_code(hipGetLastError());
       };
       if (p.kind == THIN) {
-        if (p.wide) return p.rows == 1 ? thin(k_mm_thin<A, B, W, 1>) : thin(k_mm_thin<A, B, W, 2>);
-        return p.rows == 1 ? thin(k_mm_thin<A, B, false, 1>) : thin(k_mm_thin<A, B, false, 2>);
+        auto columns = [&](auto wide, auto rows) {
+          constexpr int MT = decltype(rows)::value;
+          constexpr bool V = decltype(wide)::value;
+          return p.cols == 1 ? thin(k_mm_thin<A, B, V, MT, 1>) : thin(k_mm_thin<A, B, V, MT, 2>);
+        };
+        auto rows = [&](auto wide) {
+          return p.rows == 1 ? columns(wide, std::integral_constant<int, 1>()) : p.rows == 2 ? columns(wide, std::integral_constant<int, 2>())
+                                                                                           : columns(wide, std::integral_constant<int, 4>());
+        };
+        return p.wide ? rows(std::integral_constant<bool, W>()) : rows(std::false_type());
       }
       if (p.kind == LARGE) {
         hipLaunchKernelGGL((k_mm_large<A, B>), dim3(p.down * p.across), dim3(512), (LargeShape<A, B>::LDS), st, args, p.down, p.across);
@@ -763,7 +801,8 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
     });
   });
   if (rc != NT_OK || p.splits == 1) return rc;
-  hipLaunchKernelGGL(k_mm_join, dim3(grid_of(M * N)), dim3(256), 0, st, args, p.splits);
+  const int64_t quads = ceil_div(N, 4);
+  hipLaunchKernelGGL(k_mm_join, dim3(grid_of(M * quads)), dim3(256), 0, st, args, p.splits, (uint32_t)quads);
   return hip_code(hipGetLastError());
 }
 
