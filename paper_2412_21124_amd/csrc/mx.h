@@ -48,6 +48,16 @@ inline int check_mx(const nt_mx& m) {
   return m.ld > (1ll << 60) / m.rows || m.scale_ld > (1ll << 60) / m.rows ? NT_ERR_TOO_LARGE : NT_OK;
 }
 
+// Which of down x across tiles block b of as many takes: numbered so that the blocks that one of the eight dies is given (every eighth) are
+// neighbours, 8 rows of tiles at a time.
+__device__ inline void tile_at(uint32_t b, uint32_t total, uint32_t down, uint32_t across, int64_t& m, int64_t& n) {
+  const uint32_t each = total / 8, more = total % 8, die = b % 8;
+  const uint32_t t = b / 8 + die * each + (die < more ? die : more);
+  const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8, in = t - group * 8 * across;
+  m = first + in % high;
+  n = in / high;
+}
+
 // ---- eight elements of a lane --------------------------------------------------------------
 
 template <int DT>
@@ -188,12 +198,23 @@ __device__ inline float clamped(float x) {
   const float most = FMT == NT_MX_E2M1 ? 6.f : 448.f;
   return __builtin_amdgcn_fmed3f(x, -most, most);
 }
-template <int FMT>
+// Rounding to a format with M bits behind the leading one cuts a binary32 below bit S = 23 - M, and goes up iff what is cut is over (2 noise + 1)
+// 2^(S - 9): iff adding 2^S - 1 less that carries.  Below the least normal number 2^E codes are as far apart as in the binade behind it, so 2^E is added
+// there before and taken off behind.  That sum is exact where it counts for a 16-bit source (what it rounds off is too small to go up at all),
+// but not for an fp32 one, whose fraction is taken apart instead: 16 operations an element against 9.
+template <int FMT, bool SHORT>
 __device__ inline float chosen(float x, uint32_t noise) {
+  constexpr int M = FMT == NT_MX_E2M1 ? 1 : 3, E = FMT == NT_MX_E2M1 ? 0 : -6, S = 23 - M;
+  if (SHORT) {
+    constexpr float least = FMT == NT_MX_E2M1 ? 1.f : 0.015625f;
+    const float a = __builtin_fabsf(x), more = a < least ? least : 0.f;
+    const uint32_t carry = ((511u << (S - 9)) - 1u) - (noise << (S - 8));
+    const uint32_t bits = (__builtin_bit_cast(uint32_t, a + more) + carry) & ~((1u << S) - 1u);
+    return __builtin_copysignf(__builtin_bit_cast(float, bits) - more, x);
+  }
   const uint32_t bits = magnitude(x);
   int e = (int)(bits >> 23) - 127;
-  const int least = FMT == NT_MX_E2M1 ? 0 : -6;
-  e = (e < least ? least : e) - (FMT == NT_MX_E2M1 ? 1 : 3);
+  e = (e < E ? E : e) - M;
   const float parts = __builtin_bit_cast(float, bits) * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);   // in steps
   const float low = __builtin_floorf(parts);
   const float up = (float)noise + 0.5f < 256.f * (parts - low) ? low + 1.f : low;
@@ -222,25 +243,54 @@ __device__ inline u32x2 encode8(const float (&x)[8]) {
   }
   return r;
 }
-// Eight elements (zeros behind the row's end) of a block in four lanes: its scale byte, which all four have, and the lane's codes.
-template <int FMT, bool NOISE>
-__device__ inline u32x2 quantize8(const float (&x)[8], bool fit, const uint64_t noise, uint32_t& byte) {
+// Magnitudes of two 16-bit elements to a word, the larger of each half, and a half's bits as those of the same binary32 (NaN and infinity stay such).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t larger2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <int DT>
+__device__ inline uint32_t as_binary32(uint32_t half) {
+  if (DT == NT_BF16) return half << 16;
+  return __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)half));
+}
+// bits of the largest magnitude of eight elements
+template <int DT>
+__device__ inline uint32_t top8(const Raw<DT>& r) {
+  if (DT != NT_F32) {
+    uint32_t t = r.w[0][0] & 0x7fff7fffu;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) t = larger2(t, r.w[0][i] & 0x7fff7fffu);
+    return as_binary32<DT>((t & 0xffffu) > t >> 16 ? t & 0xffffu : t >> 16);
+  }
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t m = magnitude(x[e]);
+    const uint32_t m = magnitude(value<DT>(r, e));
     top = m > top ? m : top;
   }
-  byte = scale_byte(FMT, fit, quad_max(top));
+  return top;
+}
+// Codes of eight elements (zeros behind the row's end) of a block with this scale byte.  SHORT: of a 16-bit type.
+template <int FMT, bool NOISE, bool SHORT>
+__device__ inline u32x2 codes8(const float (&x)[8], uint32_t byte, const uint64_t noise) {
   const float by = shrink(byte == 255u ? 127u : byte);
   float y[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     y[e] = clamped<FMT>(x[e] * by);
-    if (NOISE) y[e] = chosen<FMT>(y[e], (uint32_t)(noise >> (8 * e)) & 255u);
+    if (NOISE) y[e] = chosen<FMT, SHORT>(y[e], (uint32_t)(noise >> (8 * e)) & 255u);
   }
-  u32x2 r = encode8<FMT>(y);
+  const u32x2 r = encode8<FMT>(y);
   return byte == 255u ? u32x2{0u, 0u} : r;
+}
+// Eight elements as loaded, of a block in four lanes: its scale byte, which all four have, and the lane's codes.
+template <int DT, int FMT, bool NOISE>
+__device__ inline u32x2 quantize8(const Raw<DT>& raw, bool fit, const uint64_t noise, uint32_t& byte) {
+  byte = scale_byte(FMT, fit, quad_max(top8<DT>(raw)));
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = value<DT>(raw, e);
+  return codes8<FMT, NOISE, DT != NT_F32>(x, byte, noise);
 }
 // eight values from a lane's codes, before scaling
 template <int FMT>

@@ -9,8 +9,8 @@
 #define NT_MX_THREADS 256
 #define NT_MX_TILE 128             // rows and columns of a tile that is quantised in both directions
 #define NT_MX_MOST_BLOCKS (1u << 20)
-#define NT_BWD_BLOCKS 512          // blocks that walk the rows of the norm's backward pass, each with a sum of its own for every column
-#define NT_JOIN_COLS 64            // columns and parts at a time of the kernel that adds those up
+#define NT_BWD_BLOCKS 256          // blocks that walk the rows of the norm's backward pass, each with a sum of its own for every column
+#define NT_JOIN_COLS 16            // columns and parts at a time of the kernel that adds those up
 #define NT_JOIN_PARTS 16
 #define NT_NORM_MOST_COLS 32768
 
@@ -74,11 +74,8 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_rows(QuantizeArgs a, Sprea
     const int n = left < 8 ? (int)left : 8;      // may be none or negative: the last block's end
     const Raw<DT> raw = load_n<DT>(a.src + (row * a.ld + col) * type_bytes(DT), n);
     const uint64_t noise = NOISE ? noise8(a.noise + row * a.noise_ld + col, n) : 0;
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = value<DT>(raw, e);
     uint32_t byte;
-    const u32x2 c = quantize8<FMT, NOISE>(x, a.fit, noise, byte);
+    const u32x2 c = quantize8<DT, FMT, NOISE>(raw, a.fit, noise, byte);
     store_codes<FMT>(a.codes + row * a.code_ld, octet, c);
     if ((octet & 3) == 0) a.scales[row * a.scale_ld + (octet >> 2)] = (uint8_t)byte;
   }
@@ -87,8 +84,8 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_rows(QuantizeArgs a, Sprea
 // ---------------------------------------------------------------------------------------------
 // The transpose, and both
 // ---------------------------------------------------------------------------------------------
-// A tile of 128 x 128 goes through LDS once: rows are quantised from the registers they were loaded into, columns from LDS, 32 elements to a
-// thread.  Four threads take a column's four blocks, so that a row of the transpose is written 64 or 128 bytes at a time.  Rows
+// A tile of 128 x 128 goes through LDS once: rows are quantised from the registers they were loaded into, columns from LDS, two neighbouring ones of 32
+// elements to a thread.  Four threads take a column's four blocks, so that a row of the transpose is written 64 or 128 bytes at a time.  Rows
 // in LDS are 16 bytes longer than they need, and each 32 of them begin 32 or 64 bytes further on, so that the four blocks of a column lie in
 // different banks.
 template <int DT>
@@ -100,12 +97,12 @@ struct Tile {
 };
 
 template <int DT, int FMT, int FMT_T, bool ROWS, bool NOISE>
-__global__ __launch_bounds__(NT_MX_THREADS) void k_mx_both(QuantizeArgs a, uint32_t tiles_across, int64_t tiles) {
+__global__ __launch_bounds__(NT_MX_THREADS) void k_mx_both(QuantizeArgs a, uint32_t across, int64_t tiles) {
   typedef Tile<DT> T;
   __shared__ __align__(16) uint8_t lds[T::BYTES];
   __shared__ __align__(16) uint8_t lds_noise[NOISE ? T::NOISE_BYTES : 16];
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int64_t row0 = tile / tiles_across * NT_MX_TILE, col0 = tile % tiles_across * NT_MX_TILE;
+    const int64_t row0 = tile / across * NT_MX_TILE, col0 = tile % across * NT_MX_TILE;
     constexpr int PER = NT_MX_TILE * NT_MX_TILE / 8 / NT_MX_THREADS, STEP = NT_MX_THREADS / (NT_MX_TILE / 8);
     const int c = 8 * (threadIdx.x % (NT_MX_TILE / 8)), r0 = threadIdx.x / (NT_MX_TILE / 8);
     const int64_t left = a.cols - col0 - c;
@@ -133,11 +130,8 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_both(QuantizeArgs a, uint3
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int64_t row = row0 + r0 + i * STEP;
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = value<DT>(raw[i], e);
         uint32_t byte;
-        const u32x2 codes = quantize8<FMT, NOISE>(x, a.fit, noise[i], byte);
+        const u32x2 codes = quantize8<DT, FMT, NOISE>(raw[i], a.fit, noise[i], byte);
         if (row < a.rows && octet < 4 * blocks_of(a.cols)) {
           store_codes<FMT>(a.codes + row * a.code_ld, octet, codes);
           if ((octet & 3) == 0) a.scales[row * a.scale_ld + (octet >> 2)] = (uint8_t)byte;
@@ -145,46 +139,73 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_both(QuantizeArgs a, uint3
       }
     }
     __syncthreads();
+    // two neighbouring columns to a thread: one access for both
+    const int col = 2 * (int)(threadIdx.x >> 2), block = threadIdx.x & 3;
+    constexpr int WORDS = DT == NT_F32 ? 2 : 1;
+    uint32_t w[32][WORDS], top[2] = {0u, 0u};
 #pragma unroll
-    for (int part = 0; part < NT_MX_TILE * 4 / NT_MX_THREADS; ++part) {
-      const int col = (int)(threadIdx.x >> 2) + part * (NT_MX_THREADS / 4), block = threadIdx.x & 3;
-      float x[32];
-      uint32_t top = 0;
+    for (int e = 0; e < 32; ++e) {
+      const uint8_t* p = lds + T::at(32 * block + e, col);
+      if (DT == NT_F32) {
+        const u32x2 two = *(const u32x2*)p;
+        w[e][0] = two[0];
+        w[e][WORDS - 1] = two[1];
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const uint8_t* p = lds + T::at(32 * block + e, col);
-        if (DT == NT_F32)
-          x[e] = *(const float*)p;
-        else if (DT == NT_BF16)
-          x[e] = __builtin_bit_cast(float, (uint32_t)*(const uint16_t*)p << 16);
-        else
-          x[e] = (float)*(const _Float16*)p;
-        const uint32_t m = magnitude(x[e]);
-        top = m > top ? m : top;
-      }
-      const uint32_t byte = scale_byte(FMT_T, a.fit, top);
-      const float by = shrink(byte == 255u ? 127u : byte);
-      u32x2 codes[4];
-#pragma unroll
-      for (int o = 0; o < 4; ++o) {
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          y[e] = clamped<FMT_T>(x[8 * o + e] * by);
-          if (NOISE) y[e] = chosen<FMT_T>(y[e], lds_noise[T::noise_at(32 * block + 8 * o + e, col)]);
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t m = two[k] & 0x7fffffffu;
+          top[k] = m > top[k] ? m : top[k];
         }
-        codes[o] = byte == 255u ? u32x2{0u, 0u} : encode8<FMT_T>(y);
+      } else {
+        w[e][0] = *(const uint32_t*)p;
+        top[0] = larger2(top[0], w[e][0] & 0x7fff7fffu);
       }
-      const int64_t row = col0 + col, b = row0 / 32 + block;   // of the transpose
+    }
+    if (DT != NT_F32) {
+      top[1] = as_binary32<DT>(top[0] >> 16);
+      top[0] = as_binary32<DT>(top[0] & 0xffffu);
+    }
+    u32x2 codes[2][4];
+    uint32_t byte[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) byte[k] = scale_byte(FMT_T, a.fit, top[k]);
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+      uint64_t noise2[2] = {0, 0};
+      float x[2][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = 8 * o + e;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (DT == NT_F32)
+            x[k][e] = __builtin_bit_cast(float, w[row][k * (WORDS - 1)]);
+          else if (DT == NT_BF16)
+            x[k][e] = __builtin_bit_cast(float, k ? w[row][0] & 0xffff0000u : w[row][0] << 16);
+          else
+            x[k][e] = (float)__builtin_bit_cast(_Float16, (uint16_t)(k ? w[row][0] >> 16 : w[row][0]));
+        }
+        if (NOISE) {
+          const uint32_t two = *(const uint16_t*)(lds_noise + T::noise_at(32 * block + row, col));
+          noise2[0] |= (uint64_t)(two & 255u) << (8 * e);
+          noise2[1] |= (uint64_t)(two >> 8) << (8 * e);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) codes[k][o] = codes8<FMT_T, NOISE, DT != NT_F32>(x[k], byte[k], noise2[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t row = col0 + col + k, b = row0 / 32 + block;   // of the transpose
       if (row < a.cols && b < blocks_of(a.rows)) {
         uint8_t* const to = a.codes_t + row * a.code_ld_t + b * code_bytes(FMT_T);
+        const u32x2(&c)[4] = codes[k];
         if (FMT_T == NT_MX_E2M1) {
-          *(u32x4*)to = u32x4{codes[0][0], codes[1][0], codes[2][0], codes[3][0]};
+          *(u32x4*)to = u32x4{c[0][0], c[1][0], c[2][0], c[3][0]};
         } else {
-          ((u32x4*)to)[0] = u32x4{codes[0][0], codes[0][1], codes[1][0], codes[1][1]};
-          ((u32x4*)to)[1] = u32x4{codes[2][0], codes[2][1], codes[3][0], codes[3][1]};
+          ((u32x4*)to)[0] = u32x4{c[0][0], c[0][1], c[1][0], c[1][1]};
+          ((u32x4*)to)[1] = u32x4{c[2][0], c[2][1], c[3][0], c[3][1]};
         }
-        a.scales_t[row * a.scale_ld_t + b] = (uint8_t)byte;
+        a.scales_t[row * a.scale_ld_t + b] = (uint8_t)byte[k];
       }
     }
     __syncthreads();
@@ -227,7 +248,7 @@ __device__ inline float row_sum(float x, float* scratch) {   // over the T threa
 #pragma unroll
   for (int by = 32; by; by >>= 1) x += __shfl_xor(x, by, 64);
   if (T == 64) return x;
-  const int wave = threadIdx.x / 64;
+  const int wave = threadIdx.x % T / 64;
   __syncthreads();
   if (threadIdx.x % 64 == 0) scratch[wave] = x;
   __syncthreads();
@@ -307,7 +328,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_norm(NormArgs a) {
       if (a.out && n > 0) store_n<DT>(a.out + (row * a.out_ld + col) * E, rounded<DT>(y), n);
       if (a.codes) {
         uint32_t byte;
-        const u32x2 c = a.format == NT_MX_E2M1 ? quantize8<NT_MX_E2M1, false>(y, a.fit, 0, byte) : quantize8<NT_MX_E4M3, false>(y, a.fit, 0, byte);
+        const Raw<NT_F32> exact = rounded<NT_F32>(y);
+        const u32x2 c = a.format == NT_MX_E2M1 ? quantize8<NT_F32, NT_MX_E2M1, false>(exact, a.fit, 0, byte)
+                                               : quantize8<NT_F32, NT_MX_E4M3, false>(exact, a.fit, 0, byte);
         if (col < 32 * (int)blocks_of(a.cols)) {
           if (a.format == NT_MX_E2M1)
             store_codes<NT_MX_E2M1>(a.codes + row * a.code_ld, octet, c);
@@ -329,109 +352,120 @@ struct BackwardArgs {
   int32_t cols;
 };
 
-// Blocks walk the rows.  A row is read once where its octets fit a thread's registers beside the columns' sums, else twice.
-template <int DT, int T, int V>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_backward(BackwardArgs a) {
-  constexpr int ROWS = T < 256 ? 256 / T : 1, E = type_bytes(DT);
+// Blocks walk the rows, R at a time, T threads to a row.  A row is read once where its octets fit a thread's registers beside the columns'
+// sums, else twice.  The weight is in LDS: read through the caches for every row it was 2/3 as many bytes again.  With rows side by side the chip is
+// full with 256 blocks, so that few sums are left to join (16384 x 4096 in bf16, both kernels, 137 -> 105 us, 5.1 TB/s; 512 blocks 108).
+template <int DT, int T, int V, int R>
+__global__ __launch_bounds__(T * R) void k_rms_backward(BackwardArgs a) {
+  constexpr int E = type_bytes(DT), COLS = 8 * T * V;
   constexpr bool KEEP = T * V <= 2048;
-  __shared__ float scratch[16];
-  __shared__ float joined[ROWS > 1 ? ROWS * T * V * 8 : 1];
-  const int lane = threadIdx.x % T;
+  __shared__ float scratch[R][T / 64];
+  __shared__ __align__(16) float shared[COLS];   // the weight, then the sums of rows beside the first
+  const int lane = threadIdx.x % T, beside = threadIdx.x / T;
+  for (int i = threadIdx.x; i < COLS; i += T * R) shared[i] = !a.weight ? 1.f : i < a.cols ? a.weight[i] : 0.f;
+  __syncthreads();
   float dw[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[v][e] = 0.f;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
-    Raw<DT> dy[KEEP ? V : 1], h[KEEP ? V : 1];
+  for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.rows; row0 += (int64_t)gridDim.x * R) {
+    const int64_t row = row0 + beside;
+    const bool there = row < a.rows;   // all threads take part in the sums
+    Raw<DT> dy[KEEP ? V : 1], h[KEEP ? V : 1], s[KEEP ? V : 1];
     auto load = [&](int v, Raw<DT>& y, Raw<DT>& x) {
-      const int col = 8 * (v * T + lane), n = a.cols - col;
+      const int col = 8 * (v * T + lane), n = there ? a.cols - col : 0;
       y = load_n<DT>(a.dy + (row * a.dy_ld + col) * E, n);
       x = load_n<DT>(a.h + (row * a.h_ld + col) * E, n);
     };
-    auto weight = [&](int v) {
-      Raw<NT_F32> w;
-      if (a.weight)
-        w = load_n<NT_F32>(a.weight + 8 * (v * T + lane), a.cols - 8 * (v * T + lane));
-      else
-        w.w[0] = w.w[1] = u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
-      return w;
+    auto load_sum = [&](int v, Raw<DT>& x) {
+      const int col = 8 * (v * T + lane), n = there && a.dx ? a.cols - col : 0;
+      x = load_n<DT>(a.dsum + (row * a.dsum_ld + col) * E, n);
     };
-    const float rstd = a.rstd[row];
+    auto weight = [&](int v, int e) { return shared[8 * (v * T + lane) + e]; };
+    const float rstd = there ? a.rstd[row] : 0.f;
     float inner = 0.f;
     if (KEEP) {
 #pragma unroll
       for (int v = 0; v < V; ++v) load(v, dy[KEEP ? v : 0], h[KEEP ? v : 0]);
+      if (a.dsum) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) load_sum(v, s[KEEP ? v : 0]);
+      }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!KEEP) load(v, dy[0], h[0]);
-      const Raw<NT_F32> w = weight(v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float y = value<DT>(dy[KEEP ? v : 0], e), hat = value<DT>(h[KEEP ? v : 0], e) * rstd;
-        inner = __builtin_fmaf(y * value<NT_F32>(w, e), hat, inner);
+        inner = __builtin_fmaf(y * weight(v, e), hat, inner);
         dw[v][e] = __builtin_fmaf(y, hat, dw[v][e]);
       }
     }
     if (!a.dx) continue;
-    inner = row_sum<T>(inner, scratch) / (float)a.cols;
+    inner = row_sum<T>(inner, scratch[beside]) / (float)a.cols;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = 8 * (v * T + lane), n = a.cols - col;
-      if (!KEEP) load(v, dy[0], h[0]);
-      const Raw<NT_F32> w = weight(v);
-      float d[8];
-      if (a.dsum) {
-        const Raw<DT> s = load_n<DT>(a.dsum + (row * a.dsum_ld + col) * E, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = value<DT>(s, e);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = 0.f;
+      const int col = 8 * (v * T + lane), n = there ? a.cols - col : 0;
+      if (!KEEP) {
+        load(v, dy[0], h[0]);
+        if (a.dsum) load_sum(v, s[0]);
       }
+      float d[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float hat = value<DT>(h[KEEP ? v : 0], e) * rstd;
-        d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-hat, inner, value<DT>(dy[KEEP ? v : 0], e) * value<NT_F32>(w, e)), d[e]);
+        const float hat = value<DT>(h[KEEP ? v : 0], e) * rstd, back = a.dsum ? value<DT>(s[KEEP ? v : 0], e) : 0.f;
+        d[e] = __builtin_fmaf(rstd, __builtin_fmaf(-hat, inner, value<DT>(dy[KEEP ? v : 0], e) * weight(v, e)), back);
       }
       if (n > 0) store_n<DT>(a.dx + (row * a.dx_ld + col) * E, rounded<DT>(d), n);
     }
   }
   if (!a.parts) return;
-  float* const to = a.parts + (int64_t)blockIdx.x * a.cols;
-  if (ROWS > 1) {   // waves with rows of their own: their sums one after the other
+  // the sums of the rows side by side, one after the other, through LDS to the first
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) joined[(threadIdx.x / T * V * T + v * T + lane) * 8 + e] = dw[v][e];
+  for (int r = 1; r < R; ++r) {
     __syncthreads();
-    for (int col = threadIdx.x; col < a.cols; col += 256) {
-      float x = 0.f;
+    if (beside == r) {
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) x += joined[r * V * T * 8 + col];
-      to[col] = x;
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) shared[8 * (v * T + lane) + e] = dw[v][e];
     }
-  } else {
+    __syncthreads();
+    if (beside == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int col = 8 * (v * T + lane);
+      for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (col + e < a.cols) to[col + e] = dw[v][e];
+        for (int e = 0; e < 8; ++e) dw[v][e] += shared[8 * (v * T + lane) + e];
     }
+  }
+  if (beside) return;
+  float* const to = a.parts + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int col = 8 * (v * T + lane);
+    if (col < a.cols) store_n<NT_F32>(to + col, rounded<NT_F32>(dw[v]), a.cols - col);
   }
 }
 
-// dweight <- beta dweight + scale sum over the blocks' sums: 64 columns to a block, every 16th part to a thread, joined in order
+// dweight <- beta dweight + scale sum over the blocks' sums: 16 columns to a block, every 16th part to a thread, four at a time, joined in order
 __global__ __launch_bounds__(NT_JOIN_COLS * NT_JOIN_PARTS) void k_join_columns(const float* parts, int nparts, int32_t cols, float* dweight,
                                                                                float scale, float beta) {
   __shared__ float sums[NT_JOIN_PARTS][NT_JOIN_COLS];
   const int c = threadIdx.x % NT_JOIN_COLS, p0 = threadIdx.x / NT_JOIN_COLS;
   const int64_t col = (int64_t)blockIdx.x * NT_JOIN_COLS + c;
   float x = 0.f;
-  if (col < cols)
-    for (int p = p0; p < nparts; p += NT_JOIN_PARTS) x += parts[(int64_t)p * cols + col];
+  if (col < cols) {
+    int p = p0;
+    for (; p + 3 * NT_JOIN_PARTS < nparts; p += 4 * NT_JOIN_PARTS) {
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = parts[(int64_t)(p + i * NT_JOIN_PARTS) * cols + col];
+      x += (y[0] + y[1]) + (y[2] + y[3]);
+    }
+    for (; p < nparts; p += NT_JOIN_PARTS) x += parts[(int64_t)p * cols + col];
+  }
   sums[p0][c] = x;
   __syncthreads();
   if (p0 || col >= cols) return;
@@ -471,10 +505,15 @@ int with_shape(int64_t cols, F f) {
   if (cols <= 16384) return f(Shape<1024, 2>());
   return f(Shape<1024, 4>());
 }
+// Rows side by side in a block of the backward pass: as many as 1024 threads, or their registers, allow.
+template <int T, int V>
+constexpr int rows_beside() {
+  return T == 64 ? 8 : T == 256 ? (V <= 2 ? 4 : 2) : 1;
+}
 int64_t backward_blocks(int64_t rows, int64_t cols) {
-  const int64_t groups = with_shape(cols, [&](auto s) { return (int)(s.threads < 256 ? 256 / s.threads : 1); });
-  const int64_t n = ceil_div(rows, groups);
-  return n < NT_BWD_BLOCKS ? n : NT_BWD_BLOCKS;
+  const int64_t beside = with_shape(cols, [&](auto s) { return rows_beside<decltype(s)::threads, decltype(s)::octets>(); });
+  const int64_t n = ceil_div(rows, beside), most = cols <= 1024 ? 2 * NT_BWD_BLOCKS : NT_BWD_BLOCKS;
+  return n < most ? n : most;
 }
 
 }  // namespace
@@ -605,8 +644,8 @@ int normtest_rms_norm_backward(const void* dy, int64_t dy_ld, const void* h, int
                             dy_ld, h_ld, dsum_ld, dx_ld, rows, (int32_t)cols};
     rc = with_type(dtype, [&](auto dt) {
       return with_shape(cols, [&](auto s) {
-        constexpr int T = s.threads, V = s.octets;
-        hipLaunchKernelGGL((k_rms_backward<dt(), T, V>), dim3((uint32_t)blocks), dim3(T < 256 ? 256 : T), 0, st, a);
+        constexpr int T = s.threads, V = s.octets, R = rows_beside<T, V>();
+        hipLaunchKernelGGL((k_rms_backward<dt(), T, V, R>), dim3((uint32_t)blocks), dim3(T * R), 0, st, a);
         return hip_code(hipGetLastError());
       });
     });

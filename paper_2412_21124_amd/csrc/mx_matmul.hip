@@ -362,15 +362,6 @@ __device__ inline u32x4 load_scales(const Operand& o, int64_t row, int64_t block
   return w;
 }
 
-// Which tile a block takes: numbered so that the blocks that one of the eight dies is given (every eighth) are neighbours, 8 rows of tiles at a time.
-__device__ inline void tile_at(uint32_t down, uint32_t across, int64_t& m, int64_t& n) {
-  const uint32_t total = gridDim.x, each = total / 8, more = total % 8, die = blockIdx.x % 8;
-  const uint32_t t = blockIdx.x / 8 + die * each + (die < more ? die : more);
-  const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8, in = t - group * 8 * across;
-  m = first + in % high;
-  n = in / high;
-}
-
 template <int FA, int FB, bool WIDE, int BM, int BN, int WM, int WN>
 struct TileShape {
   static constexpr int THREADS = 64 * WM * WN, STEP = step_columns<FA, FB>(), STEPS = NT_MM_CHUNK / STEP;
@@ -387,7 +378,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
 
   int64_t m0, n0;
-  tile_at(down, across, m0, n0);
+  tile_at(blockIdx.x, gridDim.x, down, across, m0, n0);
   m0 *= BM;
   n0 *= BN;
   const int64_t chunk0 = (int64_t)blockIdx.y * chunks_each, block0 = chunk0 * NT_MM_CHUNK_BLOCKS;
@@ -542,7 +533,7 @@ __global__ __launch_bounds__(512) void k_mm_large(MatmulArgs a, uint32_t down, u
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
   const int wm = wave / S::WN * (S::TILE / S::WM), wn = wave % S::WN * (S::TILE / S::WN);
   int64_t m0, n0;
-  tile_at(down, across, m0, n0);
+  tile_at(blockIdx.x, gridDim.x, down, across, m0, n0);
   m0 *= S::TILE;
   n0 *= S::TILE;
   const int32_t blocks = (int32_t)a.blocks, steps = (blocks + 3) / 4;

@@ -119,8 +119,8 @@ def test_backward(rows, cols, dtype):
         want, size, want_w, size_w = reference_backward(R.wide(dy), R.wide(h), R.wide(w) if weighted else 1.0, R.wide(rstd), R.wide(dsum) if with_sum else 0.0)
         off = (adds(cols) + 8) * STEP * size
         assert (np.abs(R.wide(dx[:, :cols]) - want) <= off + half * (np.abs(want) + off) + (6e-8 if dtype == "f16" else 0)).all()
-        # a column's sum: rows one after the other in a block, of which there are up to 512 (with up to 4 rows at a time), then those
-        serial = -(-rows // 512) + 4 + 32 + 16 + 4
+        # a column's sum: rows one after the other in a block, of which there are 256 or 512 (with up to 8 rows at a time), then those
+        serial = -(-rows // 256) + 8 + 32 + 16
         off = serial * STEP * (scale * size_w + np.abs(beta * before))
         assert (np.abs(R.wide(dw) - (scale * want_w + beta * before)) <= off).all()
         # either alone gives the same bits, dx in place of dy or dsum too
