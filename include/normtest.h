@@ -471,7 +471,9 @@ int normtest_mx_dequantize(const nt_mx* src, void* out, nt_dtype dtype, int64_t 
 
 /*
  * out (a->rows x b->rows) <- beta out + scale A B^T, summed in fp32 and rounded once to dtype; beta == 0: out is not read.  a->cols == b->cols;
- * of any formats; at most 2^22 columns, 2^31 - 1 rows and 2^21 blocks of 128 columns of out.  scale and beta: finite in fp32.  out lies apart from A and B.
+ * of any formats; at most 2^22 columns, 2^31 - 1 rows of A, 2^28 of B, 2^23 - 1 tiles of 128 x 128 in out, and where rows of codes lie over 2^22 bytes
+ * apart, 65535 times 64 rows of A.  scale and beta: finite in fp32.  out lies apart from A and B.  Scales in rows that begin at multiples of 16 bytes are read 16
+ * at a time: what stands behind a row's last one, in the same 16 bytes, may be anything.
  * For 16-bit results products of an E4M3 operand are summed by the matrix cores' 8-bit instructions, which cut each product below 2^-13 of the
  * largest of its 8 neighbours (some 3e-5 of a result); for fp32 results operands are widened to bf16 first, which
  * loses nothing but elements below 2^-133, and makes those of 2^128 and more infinite.
@@ -485,8 +487,9 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
 /*
  * h = x + residual, rounded to dtype and stored to sum_out; rstd = 1 / sqrt(mean h^2 + eps) of the stored h, per row, in fp32; y = h rstd weight,
  * rounded once: to out_mx (flags as in normtest_mx_quantize) and to out (dtype), either or both; each may be NULL, as residual (h is x), sum_out,
- * weight (fp32[cols]; 1) and rstd (fp32[rows]) may.  x, residual, sum_out and out are of one dtype, each with its own ld; sum_out may be x or
- * residual, all else lies apart.  A row with a NaN has a NaN rstd.  cols <= 32768; eps > 0 in fp32.
+ * weight (fp32[cols]; 1) and rstd (fp32[rows]) may.  Squares are summed in fp64: no finite number overflows or vanishes (an rstd below
+ * 2^-126 has fewer bits).  x, residual, sum_out and out are of one dtype, each with its own ld; sum_out may be x or residual, all else lies apart.  A row with a NaN has a NaN rstd, one with an infinity
+ * 0.  cols <= 32768; eps > 0 in fp32.
  */
 int normtest_rms_norm(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld, const float* weight, double eps,
                       nt_dtype dtype, int64_t rows, int64_t cols, void* sum_out, int64_t sum_ld, void* out, int64_t out_ld,

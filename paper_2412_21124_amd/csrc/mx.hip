@@ -241,10 +241,10 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_values(const uint8_t* code
 // ---------------------------------------------------------------------------------------------
 // RMS norm
 // ---------------------------------------------------------------------------------------------
-// T threads hold a row, V octets each, from its first reading to its codes: x and the residual are read once.  Sums are in fp32, in an order that
-// the shape alone fixes.
-template <int T>
-__device__ inline float row_sum(float x, float* scratch) {   // over the T threads of a row, in all of them; scratch: one float a wave
+// T threads hold a row, V octets each, from its first reading to its codes: x and the residual are read once.  Sums are in an order that
+// the shape alone fixes; the squares' in fp64, so that none overflows or vanishes.
+template <int T, class F>
+__device__ inline F row_sum(F x, F* scratch) {   // over the T threads of a row, in all of them; scratch: one sum a wave
 #pragma unroll
   for (int by = 32; by; by >>= 1) x += __shfl_xor(x, by, 64);
   if (T == 64) return x;
@@ -252,10 +252,16 @@ __device__ inline float row_sum(float x, float* scratch) {   // over the T threa
   __syncthreads();
   if (threadIdx.x % 64 == 0) scratch[wave] = x;
   __syncthreads();
-  float r = 0.f;
+  F r = 0;
 #pragma unroll
   for (int w = 0; w < T / 64; ++w) r += scratch[w];
   return r;
+}
+
+// 1 / sqrt(x) for a positive x: the root of x over a power of four that brings it to 1/2 .. 2
+__device__ inline float inverse_root(double x) {
+  const int half = (int)(((uint32_t)__double2hiint(x) >> 20) & 0x7ffu) / 2 - 511;   // 512 for infinity and NaN, which stay such
+  return __builtin_ldexpf(1.f / __builtin_sqrtf((float)__builtin_ldexp(x, -2 * half)), -half);
 }
 
 struct NormArgs {
@@ -267,16 +273,18 @@ struct NormArgs {
   int64_t x_ld, residual_ld, sum_ld, out_ld, code_ld, scale_ld, rows;
   int32_t cols, format, fit;
   float eps;
+  double each;   // 1 / cols
 };
 
 template <int DT, int T, int V>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_norm(NormArgs a) {
-  __shared__ float scratch[16];
+  __shared__ double scratch[16];
   constexpr int ROWS = T < 256 ? 256 / T : 1, E = type_bytes(DT);
   const int lane = threadIdx.x % T;
   constexpr bool AHEAD = T * V <= 2048;   // all of a row's loads before the first is used, where registers allow
   for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
-    float h[V][8], squares = 0.f;
+    float h[V][8];
+    double squares = 0.;
     Raw<DT> x[AHEAD ? V : 1], r[AHEAD ? V : 1];
     auto load = [&](int v) {
       const int col = 8 * (v * T + lane), n = a.cols - col;
@@ -303,10 +311,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_norm(NormArgs a) {
       }
       if (a.sum && n > 0) store_n<DT>(a.sum + (row * a.sum_ld + col) * E, stored, n);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(h[v][e], h[v][e], squares);
+      for (int e = 0; e < 8; ++e) squares = __builtin_fma((double)h[v][e], (double)h[v][e], squares);
     }
     squares = row_sum<T>(squares, scratch);
-    const float rstd = 1.f / __builtin_sqrtf(squares / (float)a.cols + a.eps);
+    const float rstd = inverse_root(__builtin_fma(squares, a.each, (double)a.eps));
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
     if (!a.out && !a.codes) continue;
 #pragma unroll
@@ -598,7 +606,7 @@ int normtest_rms_norm(const void* x, int64_t x_ld, const void* residual, int64_t
   if (cols > NT_NORM_MOST_COLS) return NT_ERR_TOO_LARGE;
   if (rows == 0 || cols == 0) return NT_OK;
   NormArgs a = {(const char*)x, (const char*)residual, weight, (char*)sum_out, (char*)out, nullptr, nullptr, rstd,
-                x_ld, residual_ld, sum_ld, out_ld, 0, 0, rows, (int32_t)cols, 0, (int32_t)(flags & NT_MX_FIT), (float)eps};
+                x_ld, residual_ld, sum_ld, out_ld, 0, 0, rows, (int32_t)cols, 0, (int32_t)(flags & NT_MX_FIT), (float)eps, 1. / (double)cols};
   if (out_mx) {
     a.codes = (uint8_t*)out_mx->codes;
     a.scales = (uint8_t*)out_mx->scales;

@@ -20,6 +20,8 @@
 #define NT_MM_THIN_TILES 96
 #define NT_MM_THIN_MANY 512        // blocks from which a wave takes 32 columns and not 16 (24 x 50257 x 768 16.4 -> 13.5 us, 1 x 16384 x 4096 8.8 -> 8.2)
 #define NT_MM_TILE_LD (1ll << 22)   // bytes from row to row that 32-bit offsets into a tile allow
+#define NT_MM_MOST_TILES ((1ll << 23) - 1)   // of a result: a launch holds less than 2^32 threads
+#define NT_MM_MOST_DOWN 65535                // groups of rows in a launch of k_mm_thin
 
 namespace {
 
@@ -689,7 +691,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
     if (ceil_div(N, 32 * beside) * p.down >= NT_MM_THIN_MANY) p.cols = 2;
     p.across = (uint32_t)ceil_div(N, 16 * p.cols * beside);
     const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(chunks, p.along);
-    if (tiles < 256) z = ceil_div(512, tiles);
+    if (tiles < 256 && ld <= NT_MM_TILE_LD) z = ceil_div(512, tiles);   // the workspace's size does not know ld, and need not
     if (z > turns) z = turns;
     p.chunks = 0;
   } else {
@@ -753,7 +755,11 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
     hipLaunchKernelGGL(k_mm_empty, dim3(grid_of(M * N)), dim3(256), 0, st, args);
     return hip_code(hipGetLastError());
   }
-  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype, a->ld > b->ld ? a->ld : b->ld, aligned16(*a) && aligned16(*b));
+  // a single row's ld means nothing, and may be anything
+  if (M == 1) args.a.ld = 0;
+  if (N == 1) args.b.ld = 0;
+  const MatmulPlan p = plan_of(M, N, K, a->format, b->format, dtype, args.a.ld > args.b.ld ? args.a.ld : args.b.ld, aligned16(*a) && aligned16(*b));
+  if (p.kind == THIN ? p.down > NT_MM_MOST_DOWN : (int64_t)p.down * p.across > NT_MM_MOST_TILES) return NT_ERR_TOO_LARGE;
   if (p.splits > 1) {
     if (!workspace || workspace_bytes < (size_t)p.splits * (size_t)M * (size_t)N * sizeof(float)) return NT_ERR_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace & 15) return NT_ERR_BAD_ARG;

@@ -89,6 +89,26 @@ def test_forward_of_zeros_nan_and_infinity():
     assert R.decode(mx.codes.cpu().numpy(), mx.format)[:, 3, 4:].any() == False       # noqa: E712  behind the last column
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [5, 700, 5003, 20000])
+def test_forward_at_the_ends_of_the_range(cols, dtype):
+    """Rows whose squares no fp32 holds."""
+    t = TYPES[dtype]
+    half = torch.finfo(t).eps / 2
+    size = torch.tensor([1e30, 3e19, 5e-20, 1e-21, 2.0 ** 124], device=DEV)[:, None]
+    x = ((torch.rand(5, cols, device=DEV) + 0.5) * size).to(t)
+    out, rstd, eps = torch.empty_like(x), torch.empty(5, device=DEV), float(np.float32(1e-41))
+    B.normtest_rms_norm(x, None, out, rstd=rstd, eps=eps)
+    wide = R.wide(x)
+    exact = 1 / np.sqrt((wide ** 2).mean(1) + eps)
+    # the sum's rounding to fp32 (halved by the root), root, reciprocal (each correct to a step); the smallest rstd is 2^-125
+    far = (0.5 + 2 + 2) * STEP
+    assert (np.abs(R.wide(rstd) - exact) <= far * exact).all()
+    y = wide * exact[:, None]
+    off = (far + 2 * STEP) * y
+    assert (np.abs(R.wide(out) - y) <= off + half * (y + off)).all()
+
+
 def reference_backward(dy, h, w, rstd, dsum):
     hat = h * rstd[:, None]
     g = dy * w

@@ -30,7 +30,7 @@ for line in sys.stdin:
     M, N, K, t = c["M"], c["N"], c.get("K", 0), c["t"]
     need = 0
     if c["call"] == "matmul":
-        a, b = mx(M, K, c["fa"], c["far"], c["odd"]), mx(N, K, c["fb"])
+        a, b = mx(M, K, c["fa"], c["far"], c["odd"]), mx(N, K, c["fb"], c.get("far_b", 0))
         need = lib.normtest_mx_matmul_workspace_bytes(i64(M), i64(N), i64(K), c["fa"], c["fb"], t)
         rc = lib.normtest_mx_matmul(a, b, dbl(1), dbl(0), vp(0x30000), t, i64(N), vp(0x40000) if need else None, size(need), None)
     elif c["call"] == "quantize":
@@ -56,14 +56,14 @@ def launches(tmp_path_factory):
     fake = str(tmp_path_factory.mktemp("fake") / "libfakehip.so")
     subprocess.run(["gcc", "-std=gnu99", "-Wall", "-Wextra", "-Werror", "-shared", "-fPIC", os.path.join(HERE, "fake_hip.c"), "-o", fake], check=True)
 
-    def run(calls):
+    def run(calls, code=0):
         out = subprocess.run([sys.executable, "-c", CLIENT, fake, B.lib()._name], check=True, capture_output=True, text=True,
                              input="".join(json.dumps(c) + "\n" for c in calls)).stdout
         got, now = [], []
         for line in out.splitlines():
             if line.startswith("rc "):
                 rc, need = map(int, line.split()[1:])
-                assert rc == 0
+                assert rc == code
                 got.append((need, now))
                 now = []
             elif re.search(r"\dk_", line):
@@ -108,6 +108,23 @@ def test_a_large_tile_is_never_split(launches):
         if kernels[0][0] == "k_mm_large":
             assert need == 0 and len(kernels) == 1, c
         assert (need > 0) == (len(kernels) == 2)
+
+
+def test_rows_far_apart(launches):
+    """The workspace that the sizes alone tell serves any distance between rows; a single row has none."""
+    got = launches([matmul(128, 128, 1 << 16, far=1 << 23), matmul(200, 300, 1 << 16, B.NT_F32, far=1 << 23, fa=0), matmul(1, 8192, 4096, far=1 << 40),
+                    dict(matmul(8192, 1, 64), far_b=1 << 40), dict(matmul(6000000, 1, 64), far_b=1 << 40)])
+    for i in (0, 1):
+        assert [k[0] for k in got[i][1]] == ["k_mm_thin"]                        # not split
+    assert got[2] == launches([matmul(1, 8192, 4096)])[0]
+    assert got[3] == launches([matmul(8192, 1, 64)])[0] and got[3][1][0][0] == "k_mm_tile"
+    assert got[4] == launches([matmul(6000000, 1, 64)])[0]
+
+
+def test_more_blocks_than_a_launch_takes(launches):
+    many = matmul((1 << 31) - 1, 1, 64)
+    assert launches([many], B.NT_ERR_TOO_LARGE)[0][1] == []
+    assert launches([dict(matmul(1 << 23, 2, 64), far_b=1 << 23)], B.NT_ERR_TOO_LARGE)[0][1] == []
 
 
 def test_quantize_and_norm(launches):
