@@ -48,11 +48,15 @@ inline int check_mx(const nt_mx& m) {
   return m.ld > (1ll << 60) / m.rows || m.scale_ld > (1ll << 60) / m.rows ? NT_ERR_TOO_LARGE : NT_OK;
 }
 
+// A number for block b of `total`, so that the blocks that one of the eight dies is given (every eighth) have neighbouring ones.
+__device__ inline uint32_t by_die(uint32_t b, uint32_t total) {
+  const uint32_t each = total / 8, more = total % 8, die = b % 8;
+  return b / 8 + die * each + (die < more ? die : more);
+}
 // Which of down x across tiles block b of as many takes: numbered so that the blocks that one of the eight dies is given (every eighth) are
 // neighbours, 8 rows of tiles at a time.
 __device__ inline void tile_at(uint32_t b, uint32_t total, uint32_t down, uint32_t across, int64_t& m, int64_t& n) {
-  const uint32_t each = total / 8, more = total % 8, die = b % 8;
-  const uint32_t t = b / 8 + die * each + (die < more ? die : more);
+  const uint32_t t = by_die(b, total);
   const uint32_t group = t / (8 * across), first = group * 8, high = down - first < 8 ? down - first : 8, in = t - group * 8 * across;
   m = first + in % high;
   n = in / high;

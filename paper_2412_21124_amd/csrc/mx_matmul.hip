@@ -167,14 +167,18 @@ __device__ inline uint32_t by_step(uint32_t w, int g) {
 // ---------------------------------------------------------------------------------------------
 // Few rows
 // ---------------------------------------------------------------------------------------------
-// A wave takes NT x 16 columns of the result and MT x 16 rows, straight from memory to registers, a chunk of 512 columns of A and B at a time.  `along` of
-// a block's four waves (and blockIdx.z) share out the chunks, and are joined through LDS; the others have columns of their own.  Lanes that hold pieces
-// of one row load 64 bytes of it side by side, and one word of scales each, which then change places.  (Four blocks of a lane side by
-// side need no change, but every lane loads from a cache line of its own: 24 x 50257 x 768 19.7 us.)
-template <int F, bool WIDE>
+// A wave takes NT x 16 columns of the result and MT x 16 rows, straight from memory to registers, U x 128 columns of A and B at a time.  `along` of
+// a block's four waves (and blockIdx.z) share those out, and are joined through LDS; the others have columns of their own.  Lanes that hold pieces
+// of one row load 64 bytes of it side by side, and one word of scales each, for 512 columns, which then change places.  (Four blocks of a lane side by
+// side need no change, but every lane loads from a cache line of its own: 24 x 50257 x 768 19.7 us.)  Bound by memory where there is one row (1 x 16384 x
+// 4096 8.2 us, 4.4 TB/s), by the time of a wave, load to last product, where there are more.  Hence U = 2 for fewer than 2048 columns: 24 x 50257 x 768 13.4 ->
+// 12.7, of 1536 21.7 -> 19.6 (8 x 50257 x 1024 8.4 -> 8.7).  Blocks side by side are on one die, where the lines that they share are written once: 12.7 -> 12.2,
+// the single row 8.4 to 8.8 -> 8.2.
+template <int F, bool WIDE, int U>
 struct Chunk {
-  Frag<F> f[4];
+  Frag<F> f[U];
   uint32_t scales;
+  int shift;        // of the scales: 16 where U is 2 and this is the upper half of what one word holds
   __device__ inline void load(const Operand& o, int64_t row, int64_t block0, int64_t blocks, bool whole) {
     const int g = (threadIdx.x & 63) / 16;
     const bool there = row < o.rows;
@@ -185,7 +189,7 @@ struct Chunk {
       return x;
     };
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       const int64_t first = block0 + 4 * u;
       if (F == NT_MX_E2M1) {
         f[u].w[0] = piece(first + g, 0);
@@ -198,10 +202,10 @@ struct Chunk {
       }
     }
     uint32_t word = 0;
-    const int64_t b0 = block0 + 4 * g;
+    const int64_t b0 = block0 / 16 * 16 + 4 * g;   // of all 512
     if (there) {
       const uint8_t* const s = o.scales + row * o.scale_ld;
-      if (whole || b0 + 4 <= blocks) {
+      if (b0 + 4 <= blocks) {
         word = *(const u32_any*)(s + b0);
       } else {
         for (int u = 0; u < 3; ++u)
@@ -209,27 +213,28 @@ struct Chunk {
       }
     }
     scales = word;
+    shift = U == 4 ? 0 : (int)(block0 & 8) * 2;
   }
   // where the scales are needed: what the lane loaded is its neighbours'
-  __device__ inline void settle() { scales = by_step(scales, (threadIdx.x & 63) / 16); }
+  __device__ inline void settle() { scales = by_step(scales, (threadIdx.x & 63) / 16) >> shift; }
 };
 
-template <int FA, int FB, bool WIDE, int MT, int NT>
+template <int FA, int FB, bool WIDE, int MT, int NT, int U>
 __global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a, int along) {
   __shared__ f32x4 sums[NT_MM_THIN_WAVES][MT * NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, r = lane % 16, part = wave % along;
-  const int64_t n0 = ((int64_t)blockIdx.x * (NT_MM_THIN_WAVES / along) + wave / along) * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
+  const int64_t n0 = ((int64_t)by_die(blockIdx.x, gridDim.x) * (NT_MM_THIN_WAVES / along) + wave / along) * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int64_t chunks = (a.blocks + NT_MM_CHUNK_BLOCKS - 1) / NT_MM_CHUNK_BLOCKS, step = (int64_t)gridDim.z * along;
+  const int64_t chunks = (a.blocks + 4 * U - 1) / (4 * U), step = (int64_t)gridDim.z * along;
   for (int64_t c = (int64_t)blockIdx.z * along + part; c < chunks; c += step) {
-    const int64_t block0 = c * NT_MM_CHUNK_BLOCKS;
-    const bool whole = block0 + NT_MM_CHUNK_BLOCKS <= a.blocks;
-    Chunk<FB, WIDE> b[NT];
-    Chunk<FA, WIDE> x[MT];
+    const int64_t block0 = c * (4 * U);
+    const bool whole = block0 + 4 * U <= a.blocks;
+    Chunk<FB, WIDE, U> b[NT];
+    Chunk<FA, WIDE, U> x[MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) b[n].load(a.b, n0 + 16 * n + r, block0, a.blocks, whole);
 #pragma unroll
@@ -245,12 +250,14 @@ __global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a,
         for (int n = 0; n < NT; ++n) {
           acc[t][n] = multiply<FA, FB, 0>(b[n].f[0], b[n].scales, x[t].f[0], x[t].scales, acc[t][n]);
           acc[t][n] = multiply<FA, FB, 1>(b[n].f[1], b[n].scales, x[t].f[1], x[t].scales, acc[t][n]);
-          acc[t][n] = multiply<FA, FB, 2>(b[n].f[2], b[n].scales, x[t].f[2], x[t].scales, acc[t][n]);
-          acc[t][n] = multiply<FA, FB, 3>(b[n].f[3], b[n].scales, x[t].f[3], x[t].scales, acc[t][n]);
+          if constexpr (U == 4) {
+            acc[t][n] = multiply<FA, FB, 2>(b[n].f[2], b[n].scales, x[t].f[2], x[t].scales, acc[t][n]);
+            acc[t][n] = multiply<FA, FB, 3>(b[n].f[3], b[n].scales, x[t].f[3], x[t].scales, acc[t][n]);
+          }
         }
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           bf16x8 wb[NT];
@@ -670,7 +677,7 @@ __global__ __launch_bounds__(512) void k_mm_large(MatmulArgs a, uint32_t down, u
 enum { THIN, MIDDLE, LARGE };
 struct MatmulPlan {
   bool wide;
-  int kind, rows, cols, along;   // of THIN: 16-row and 16-column groups of a wave, and the block's waves that share chunks
+  int kind, rows, cols, along, steps;   // of THIN: 16-row and 16-column groups of a wave, the block's waves that share columns, and 128s at a time
   uint32_t down, across; // tiles
   int splits, chunks;    // parts of the columns, and chunks of 512 in each
 };
@@ -681,7 +688,9 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
   p.wide = dtype == NT_F32 && (fa == NT_MX_E4M3 || fb == NT_MX_E4M3);
   const int64_t chunks = ceil_div(K, NT_MM_CHUNK);
   p.rows = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-  p.along = chunks >= 4 ? 4 : chunks >= 2 ? 2 : 1;
+  p.steps = chunks < 4 ? 2 : 4;
+  const int64_t pieces = ceil_div(K, 128 * p.steps);
+  p.along = pieces > 2 ? 4 : pieces == 2 ? 2 : 1;
   p.cols = 1;
   int64_t z = 1;
   if (M <= NT_MM_THIN_ROWS || (M <= NT_MM_THIN_MORE_ROWS && ceil_div(N, 128) < NT_MM_THIN_TILES) || ld > NT_MM_TILE_LD) {
@@ -690,7 +699,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, int fa, int fb, int dtype, i
     p.down = (uint32_t)ceil_div(M, 16 * p.rows);
     if (ceil_div(N, 32 * beside) * p.down >= NT_MM_THIN_MANY) p.cols = 2;
     p.across = (uint32_t)ceil_div(N, 16 * p.cols * beside);
-    const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(chunks, p.along);
+    const int64_t tiles = (int64_t)p.across * p.down, turns = ceil_div(pieces, p.along);
     if (tiles < 256 && ld <= NT_MM_TILE_LD) z = ceil_div(512, tiles);   // the workspace's size does not know ld, and need not
     if (z > turns) z = turns;
     p.chunks = 0;
@@ -781,7 +790,8 @@ int normtest_mx_matmul(const nt_mx* a, const nt_mx* b, double scale, double beta
         auto columns = [&](auto wide, auto rows) {
           constexpr int MT = decltype(rows)::value;
           constexpr bool V = decltype(wide)::value;
-          return p.cols == 1 ? thin(k_mm_thin<A, B, V, MT, 1>) : thin(k_mm_thin<A, B, V, MT, 2>);
+          return p.cols == 1 ? (p.steps == 2 ? thin(k_mm_thin<A, B, V, MT, 1, 2>) : thin(k_mm_thin<A, B, V, MT, 1, 4>))
+                             : (p.steps == 2 ? thin(k_mm_thin<A, B, V, MT, 2, 2>) : thin(k_mm_thin<A, B, V, MT, 2, 4>));
         };
         auto rows = [&](auto wide) {
           return p.rows == 1 ? columns(wide, std::integral_constant<int, 1>()) : p.rows == 2 ? columns(wide, std::integral_constant<int, 2>())

@@ -263,3 +263,30 @@ def test_product_repeats():
     first = B.normtest_mx_matmul(a, b, dtype=torch.float32)
     for _ in range(5):
         assert torch.equal(B.normtest_mx_matmul(a, b, dtype=torch.float32), first)
+
+
+@pytest.mark.parametrize("form,form_b", KINDS, ids="-".join)
+@pytest.mark.parametrize("M,N,K", [(1, 16500, 600), (24, 16450, 1290), (7, 16390, 2100), (30, 33000, 40)], ids=lambda v: str(v))
+def test_product_of_few_rows_and_many_columns(M, N, K, form, form_b):
+    for k, dtype in enumerate(("bf16", "f32")):
+        check_product(operand(M, K, form, M + K + k), operand(N, K, form_b, N + K + k, pad=k), dtype, 0.5, 1.0, pad=1 - k)
+
+
+@pytest.mark.parametrize("form,form_b", KINDS, ids="-".join)
+def test_product_of_rows_far_apart(form, form_b):
+    """Over 4 MB from row to row: beyond the offsets that tiles load with.  A single row's distance means nothing."""
+    far = (1 << 22) + 16
+
+    def apart(m, rows_apart):
+        codes = torch.empty(m.rows, rows_apart, dtype=torch.uint8, device=DEV)[:, : m.codes.shape[1]]
+        return B.MxTensor(codes.copy_(m.codes), m.scales, m.cols, m.format)
+
+    for k, (M, N, K, dtype) in enumerate([(130, 70, 1100, "f32"), (33, 300, 5000, "bf16"), (5, 90, 700, "f32")]):
+        a, b = operand(M, K, form, k), operand(N, K, form_b, k + 50)
+        for x, y in ((apart(a, far), b), (a, apart(b, far)), (apart(a, far), apart(b, far))):
+            check_product(x, y, dtype)
+    one, many = operand(1, 600, form, 3), operand(300, 600, form_b, 4)
+    codes = torch.as_strided(one.codes, one.codes.shape, (1 << 40, 1))
+    same = B.MxTensor(codes, one.scales, 600, one.format)
+    assert torch.equal(B.normtest_mx_matmul(same, many), B.normtest_mx_matmul(one, many))
+    assert torch.equal(B.normtest_mx_matmul(many, same), B.normtest_mx_matmul(many, one))

@@ -78,11 +78,11 @@ def launches(tmp_path_factory):
 def test_few_rows(launches):
     got = launches([matmul(1, 16384, 4096), matmul(16, 64, 512), matmul(17, 50257, 768, B.NT_F32), matmul(32, 100, 100), matmul(64, 2048, 2048),
                     matmul(1, 16, 1 << 20, fa=0)])
-    assert got[0] == (0, [("k_mm_thin", [1, 0, 0, 1, 2], 512, 256, 0)])
-    assert got[1] == (0, [("k_mm_thin", [1, 0, 0, 1, 1], 1, 256, 0)])
-    assert got[2] == (0, [("k_mm_thin", [1, 0, 1, 2, 2], 786, 256, 0)])       # fp32 with an 8-bit operand: widened
-    assert got[3] == (0, [("k_mm_thin", [1, 0, 0, 2, 1], 2, 256, 0)])
-    assert got[4] == (0, [("k_mm_thin", [1, 0, 0, 4, 1], 128, 256, 0)])
+    assert got[0] == (0, [("k_mm_thin", [1, 0, 0, 1, 2, 4], 512, 256, 0)])
+    assert got[1] == (0, [("k_mm_thin", [1, 0, 0, 1, 1, 2], 2, 256, 0)])
+    assert got[2] == (0, [("k_mm_thin", [1, 0, 1, 2, 2, 2], 1571, 256, 0)])       # fp32 with an 8-bit operand: widened
+    assert got[3] == (0, [("k_mm_thin", [1, 0, 0, 2, 1, 2], 2, 256, 0)])
+    assert got[4] == (0, [("k_mm_thin", [1, 0, 0, 4, 1, 4], 128, 256, 0)])
     need, kernels = got[5]
     assert [k[0] for k in kernels] == ["k_mm_thin", "k_mm_join"] and need == 512 * 16 * 4
 
