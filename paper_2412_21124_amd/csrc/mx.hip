@@ -258,10 +258,16 @@ __device__ inline F row_sum(F x, F* scratch) {   // over the T threads of a row,
   return r;
 }
 
-// 1 / sqrt(x) for a positive x: the root of x over a power of four that brings it to 1/2 .. 2
-__device__ inline float inverse_root(double x) {
+// 1 / sqrt(x) for a positive x, as the nearest fp32 number and what is left of it: in fp32 of the x over a power of four that lies in 1/2 .. 2, then
+// one of Newton's steps in fp64.
+__device__ inline float inverse_root(double x, float& rest) {
   const int half = (int)(((uint32_t)__double2hiint(x) >> 20) & 0x7ffu) / 2 - 511;   // 512 for infinity and NaN, which stay such
-  return __builtin_ldexpf(1.f / __builtin_sqrtf((float)__builtin_ldexp(x, -2 * half)), -half);
+  const float near = __builtin_ldexpf(1.f / __builtin_sqrtf((float)__builtin_ldexp(x, -2 * half)), -half);
+  rest = 0.f;
+  if (half == 512) return near;
+  const double r = near * (1.5 - 0.5 * (x * near * near));
+  rest = (float)(r - (float)r);
+  return (float)r;
 }
 
 struct NormArgs {
@@ -314,20 +320,23 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_norm(NormArgs a) {
       for (int e = 0; e < 8; ++e) squares = __builtin_fma((double)h[v][e], (double)h[v][e], squares);
     }
     squares = row_sum<T>(squares, scratch);
-    const float rstd = inverse_root(__builtin_fma(squares, a.each, (double)a.eps));
+    float rest;
+    const float rstd = inverse_root(__builtin_fma(squares, a.each, (double)a.eps), rest);
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
     if (!a.out && !a.codes) continue;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int octet = v * T + lane, col = 8 * octet, n = a.cols - col;
       float y[8];
-      if (a.weight) {
-        const Raw<NT_F32> w = load_n<NT_F32>(a.weight + col, n);
+      // h (rstd + rest) as a number and what is left, times the weight: rounded once.  (Twice, and with a rounded rstd, moves
+      // more elements across a border of their codes; the operations hide behind memory.)
+      const Raw<NT_F32> w = a.weight ? load_n<NT_F32>(a.weight + col, n) : Raw<NT_F32>();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = h[v][e] * rstd * value<NT_F32>(w, e);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = h[v][e] * rstd;
+      for (int e = 0; e < 8; ++e) {
+        const float by = a.weight ? value<NT_F32>(w, e) : 1.f, top = h[v][e] * rstd;
+        const float low = __builtin_fmaf(h[v][e], rest, __builtin_fmaf(h[v][e], rstd, -top));
+        const float all = __builtin_fmaf(top, by, low * by);
+        y[e] = all == all ? all : top * by;   // an infinite weight's 0 inf is none of the formula
       }
       if (n < 8) {   // behind the row's end: zero codes, also where rstd is infinite or NaN
 #pragma unroll

@@ -109,6 +109,26 @@ def test_forward_at_the_ends_of_the_range(cols, dtype):
     assert (np.abs(R.wide(out) - y) <= off + half * (y + off)).all()
 
 
+@pytest.mark.parametrize("cols", [3, 768, 4096, 20000])
+def test_forward_rounds_once(cols):
+    gen = torch.Generator().manual_seed(cols)
+    x, w = torch.randn(64, cols, generator=gen).to(DEV), (1 + 0.1 * torch.randn(cols, generator=gen)).to(DEV)
+    for weight in (w, None):
+        out, rstd = torch.empty_like(x), torch.empty(64, device=DEV)
+        B.normtest_rms_norm(x, weight, out, rstd=rstd, eps=EPS)
+        wide = R.wide(x)
+        exact = 1 / np.sqrt((wide ** 2).mean(1) + np.float32(EPS))
+        # half a step each, and 2^-40 for what the second words leave
+        assert (np.abs(R.wide(rstd) - exact) <= STEP * exact * (1 + 2.0 ** -16)).all()
+        y = wide * exact[:, None] * (R.wide(w) if weight is not None else 1.0)
+        assert (np.abs(R.wide(out) - y) <= STEP * np.abs(y) * (1 + 2.0 ** -16)).all()
+    w[1] = float("inf")
+    w[2] = 0
+    out = torch.empty_like(x)
+    B.normtest_rms_norm(x, w, out)
+    assert torch.equal(out[:, 1], torch.sign(x[:, 1]) * float("inf")) and (out[:, 2] == 0).all()
+
+
 def reference_backward(dy, h, w, rstd, dsum):
     hat = h * rstd[:, None]
     g = dy * w
