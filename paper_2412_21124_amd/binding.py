@@ -853,7 +853,9 @@ class MxTensor:
     """A microscaled matrix: rows x cols elements in 4 bits (NT_MX_E2M1) or 8 (NT_MX_E4M3), 32 of a row to a scale.
 
     codes, scales: uint8 device tensors with a row for every row, of at least ceil(cols / 32) blocks' codes (16 or 32 bytes each; rows begin at
-    multiples of 16 bytes) and that many scales.  Elements behind column cols in a row's last block are zero codes.  make_mx allocates one."""
+    multiples of 16 bytes) and that many scales.  Elements behind column cols in a row's last block are zero codes.  make_mx allocates one.
+    It stays the matrix of the tensors it was made of, whose bytes may change: its attributes are not assigned, and a call on one whose tensors
+    have other memory or another shape by now raises."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, format: int = NT_MX_E2M1):
         if format not in _MX_BLOCK_BYTES:
@@ -882,6 +884,11 @@ class MxTensor:
         self._made_of = _place(codes), _place(scales)
         lib()
         self.native = _fast and _fast.make_mx(codes, scales, self.rows, cols, ld, scale_ld, format) or None   # as the native call path knows it
+
+    def __setattr__(self, name, value):
+        if "native" in self.__dict__:   # the last one: whole.  What the calls know this matrix by would not follow
+            raise AttributeError("a microscaled matrix stays what it was made as: make another MxTensor for other %s" % name)
+        super().__setattr__(name, value)
 
     @property
     def shape(self):

@@ -273,6 +273,20 @@ struct List {
   PyObject* owner;   // of the plan's record
 };
 int64_t kind_of(const at::Tensor& t) { return (int64_t)t.scalar_type() << 32 | t.dim(); }
+void note(std::vector<int64_t>& were, const at::Tensor& t) {
+  were.insert(were.end(), {(int64_t)(intptr_t)t.data_ptr(), kind_of(t)});
+  were.insert(were.end(), t.sizes().begin(), t.sizes().end());
+  were.insert(were.end(), t.strides().begin(), t.strides().end());
+}
+// Whether t is what was noted, and on to the next one's notes.
+bool as_noted(const at::Tensor& t, const int64_t*& was) {
+  if ((int64_t)(intptr_t)t.data_ptr() != was[0] || kind_of(t) != was[1]) return false;
+  was += 2;
+  for (const auto& now : {t.sizes(), t.strides()})
+    for (const int64_t x : now)
+      if (x != *was++) return false;
+  return true;
+}
 const char list_name[] = "normtest.list";
 void list_free(PyObject* capsule) {
   List* l = (List*)PyCapsule_GetPointer(capsule, list_name);
@@ -288,10 +302,7 @@ PyObject* make_list(PyObject*, PyObject* const* a, Py_ssize_t n) {
     l->all_f32 = true;
     for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
       l->tensors.push_back(tensor(PyTuple_GET_ITEM(a[0], i)));
-      const at::Tensor& t = l->tensors.back();
-      l->were.insert(l->were.end(), {(int64_t)(intptr_t)t.data_ptr(), kind_of(t)});
-      l->were.insert(l->were.end(), t.sizes().begin(), t.sizes().end());
-      l->were.insert(l->were.end(), t.strides().begin(), t.strides().end());
+      note(l->were, l->tensors.back());
       l->all_f32 = l->all_f32 && l->tensors.back().scalar_type() == at::kFloat;
     }
     l->plan = entry<const nt_plan>(a[1]);
@@ -314,13 +325,8 @@ const List* held(PyObject* o) {
 }
 bool same(const List& l) {
   const int64_t* was = l.were.data();
-  for (const at::Tensor& t : l.tensors) {
-    if ((int64_t)(intptr_t)t.data_ptr() != was[0] || kind_of(t) != was[1]) return false;
-    was += 2;
-    for (const auto& now : {t.sizes(), t.strides()})
-      for (const int64_t x : now)
-        if (x != *was++) return false;
-  }
+  for (const at::Tensor& t : l.tensors)
+    if (!as_noted(t, was)) return false;
   return true;
 }
 // The list behind a capsule, its tensors what its table says; `first`: the list whose plan it has to share.
@@ -416,9 +422,10 @@ PyObject* adamw_tensors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- microscaled matrices and the norm ----
-// A microscaled matrix as the binding made it: its bytes, where they were then, and the library's record.
+// A microscaled matrix as the binding made it: its bytes, what they were then (as of a list's tensors), and the library's record.
 struct Mx {
   at::Tensor codes, scales;
+  std::vector<int64_t> were;
   nt_mx record;
   c10::Device device = c10::Device(c10::DeviceType::CPU);
 };
@@ -430,6 +437,8 @@ PyObject* make_mx(PyObject*, PyObject* const* a, Py_ssize_t n) {
     std::unique_ptr<Mx> m(new Mx());
     m->codes = tensor(a[0]);
     m->scales = tensor(a[1]);
+    note(m->were, m->codes);
+    note(m->were, m->scales);
     m->device = m->codes.device();
     m->record = {m->codes.data_ptr(), m->scales.data_ptr(), integer(a[2]), integer(a[3]), integer(a[4]), integer(a[5]), small(a[6]), 0};
     PyObject* capsule = PyCapsule_New(m.get(), mx_name, mx_free);
@@ -438,12 +447,12 @@ PyObject* make_mx(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return capsule;
   });
 }
-// The matrix behind a capsule, its bytes where they were, rows x cols (negative: any) on this device.
+// The matrix behind a capsule, its bytes what they were, rows x cols (negative: any) on this device.
 const nt_mx* mx_of(PyObject* o, const c10::Device& device, int64_t rows, int64_t cols) {
   if (!PyCapsule_IsValid(o, mx_name)) throw Refused();
   const Mx& m = *(const Mx*)PyCapsule_GetPointer(o, mx_name);
-  if (m.device != device || m.codes.data_ptr() != m.record.codes || m.scales.data_ptr() != m.record.scales || m.codes.size(0) != m.record.rows ||
-      m.scales.size(0) != m.record.rows || (rows >= 0 && (m.record.rows != rows || m.record.cols != cols)))
+  const int64_t* was = m.were.data();
+  if (m.device != device || !as_noted(m.codes, was) || !as_noted(m.scales, was) || (rows >= 0 && (m.record.rows != rows || m.record.cols != cols)))
     throw Refused();
   return &m.record;
 }
