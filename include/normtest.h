@@ -458,8 +458,9 @@ enum { NT_MX_FIT = 1u };   /* the least scale under which no element of the bloc
  * Quantise src (rows x cols numbers).  For a block with largest magnitude a, the scale is 2^s, s = floor(log2 a) - 2 (E2M1) or - 8 (E4M3),
  * under which an a of over 1.5 or 1.75 times a power of two is clamped to the largest code, or with NT_MX_FIT the least s for which a <= 6
  * (448) 2^s; s is held in -127 .. 127, and is -127 for a block of zeros.  Elements are x 2^-s rounded to nearest even, or, with `noise`
- * (device bytes, rows x cols, noise_ld apart), away from zero iff noise + 1/2 < 256 times the fraction: an unbiased rounding, to 2^-9 of a step, for bytes
- * drawn uniformly.  A block that holds a NaN or an infinity becomes NaN (scale byte 255).
+ * (device bytes, rows x cols, noise_ld apart), away from zero iff noise + 1/2 < 256 times the fraction.  With NT_MX_FIT that is an unbiased rounding, to
+ * 2^-9 of a step, for bytes drawn uniformly.  Without it elements over the largest code are not: they are clamped to it, whatever their bytes, and lose up to
+ * a quarter (E2M1) or an eighth (E4M3). A block that holds a NaN or an infinity becomes NaN (scale byte 255).
  * out: rows x cols, or NULL.  out_t: cols x rows, the transpose (blocks of 32 rows of src, the same noise for an element), or NULL.  One of
  * them at least; of any formats.  Bytes of a row of codes from its last block's end up to ld are left as they are.
  */

@@ -969,7 +969,8 @@ def normtest_mx_quantize(src: torch.Tensor, out: Optional[MxTensor] = None, out_
 
     A block's scale is the power of two of its largest magnitude, under which that one may be clamped to the format's largest number (6 or
     448), or with `fit` the least that clamps nothing.  noise: uint8, src's shape; a random byte for every element rounds it up with the
-    probability of its fraction instead of to nearest even.  A block with a NaN or an infinity reads as NaN."""
+    probability of its fraction instead of to nearest even: without bias if `fit` is given, as what is clamped is too small whatever its byte.
+    A block with a NaN or an infinity reads as NaN."""
     where = "normtest_mx_quantize"
     if stream is None and _fast and _done(_fast.mx_quantize(_lib.normtest_mx_quantize_entry, src, _native_mx(out), _native_mx(out_t), fit, noise), where):
         return
