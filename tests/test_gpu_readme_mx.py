@@ -45,3 +45,21 @@ def test_gradients_are_rounded_without_bias(monkeypatch):
         a = np.abs(want) / scale
         step = np.diff(R.GRID[R.E4M3])[np.minimum(np.searchsorted(R.GRID[R.E4M3], a, side="right") - 1, 125)] * scale
         assert (np.abs(total / 256 - want) <= step / 512 * (1 + 1e-9)).all()
+
+
+def test_gradients_are_means_of_the_micro_batches():
+    """The weight's and the norm's gradient of a few micro-batches, added up in what the recipe is given, against 64 bits."""
+    s = inputs(2)
+    want_w, want_n, size_w, size_n = 0.0, 0.0, 0.0, 0.0
+    for k in range(s["micro_batches"]):
+        s.update({name: value for name, value in inputs(3 + k).items() if name in ("x", "r", "dy", "dh")})
+        exec(RECIPE, s)
+        turned, y = R.numbers(s["G8t"]), R.numbers(s["X8t"])
+        term = R.wide(s["dxn"]) * R.wide(s["h"]) * R.wide(s["rstd"])[:, None]
+        want_w, size_w = want_w + turned @ y.T, size_w + np.abs(turned) @ np.abs(y).T
+        want_n, size_n = want_n + term.sum(0), size_n + np.abs(term).sum(0)
+    n = s["micro_batches"]
+    # fp32 sums: for a micro-batch, two instructions' 32 tokens and the joins of parts, a cut of 2^-23 each (some 18), or 64 rows' additions and products
+    # of 2^-24 each (some 80), and two roundings as it is scaled and added to the others
+    assert (np.abs(R.wide(s["weight_grad"]) - want_w / n) <= 24 * 2.0 ** -23 * size_w / n).all()
+    assert (np.abs(R.wide(s["norm_grad"]) - want_n / n) <= 96 * 2.0 ** -24 * size_n / n).all()
