@@ -491,7 +491,7 @@ int normtest_mx_matmul_full(const nt_mx* a, const nt_mx* b, double scale, double
 
 /*
  * h = x + residual, rounded to dtype and stored to sum_out; rstd = 1 / sqrt(mean h^2 + eps) of the stored h, per row, in fp32; y = h rstd weight,
- * rounded once: to out_mx (flags as in normtest_mx_quantize) and to out (dtype), either or both; each may be NULL, as residual (h is x), sum_out,
+ * rounded once to fp32, and from there to out_mx (flags as in normtest_mx_quantize) and to out (dtype), either or both; each may be NULL, as residual (h is x), sum_out,
  * weight (fp32[cols]; 1) and rstd (fp32[rows]) may.  Squares are summed in fp64: no finite number overflows or vanishes (an rstd below
  * 2^-126 has fewer bits).  x, residual, sum_out and out are of one dtype, each with its own ld; sum_out may be x or residual, all else lies apart.  A row with a NaN has a NaN rstd, one with an infinity
  * 0.  cols <= 32768; eps > 0 in fp32.

@@ -334,8 +334,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_rms_norm(NormArgs a) {
     for (int v = 0; v < V; ++v) {
       const int octet = v * T + lane, col = 8 * octet, n = a.cols - col;
       float y[8];
-      // h (rstd + rest) as a number and what is left, times the weight: rounded once.  (Twice, and with a rounded rstd, moves
-      // more elements across a border of their codes; the operations hide behind memory.)
+      // h (rstd + rest) as a number and what is left, times the weight: rounded once to fp32, which `rounded` and quantize8 start from.  (Twice, and
+      // with a rounded rstd, moves more elements across a border of their codes; the operations hide behind memory.)
       const Raw<NT_F32> w = a.weight ? load_n<NT_F32>(a.weight + col, n) : Raw<NT_F32>();
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
