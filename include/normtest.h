@@ -460,9 +460,9 @@ enum { NT_MX_FIT = 1u };   /* the least scale under which no element of the bloc
  * (448) 2^s; s is held in -127 .. 127, and is -127 for a block of zeros.  Elements are x 2^-s rounded to nearest even, or, with `noise`
  * (device bytes, rows x cols, noise_ld apart), away from zero iff noise + 1/2 < 256 times the fraction.  With NT_MX_FIT that is an unbiased rounding, to
  * 2^-9 of a step, for bytes drawn uniformly.  Without it elements over the largest code are not: they are clamped to it, whatever their bytes, and lose up to
- * a quarter (E2M1) or an eighth (E4M3). A block that holds a NaN or an infinity becomes NaN (scale byte 255).
+ * a quarter (E2M1) or an eighth (E4M3).  A block that holds a NaN or an infinity becomes NaN (scale byte 255).
  * out: rows x cols, or NULL.  out_t: cols x rows, the transpose (blocks of 32 rows of src, the same noise for an element), or NULL.  One of
- * them at least; of any formats.  Bytes of a row of codes from its last block's end up to ld are left as they are.
+ * them at least; of any formats, and apart from src, noise and one another.  Bytes of a row of codes from its last block's end up to ld are left as they are.
  */
 int normtest_mx_quantize(const void* src, nt_dtype dtype, int64_t rows, int64_t cols, int64_t ld, const uint8_t* noise,
                          int64_t noise_ld, const nt_mx* out, const nt_mx* out_t, uint32_t flags, void* hip_stream);

@@ -978,6 +978,9 @@ def normtest_mx_quantize(src: torch.Tensor, out: Optional[MxTensor] = None, out_
     (rows, cols), dev = src.shape, src.device
     if out is None and out_t is None:
         raise ValueError("%s needs out, out_t or both" % where)
+    if isinstance(out, MxTensor) and isinstance(out_t, MxTensor) and out.rows * out.cols > 0 and (
+            out.codes.data_ptr() == out_t.codes.data_ptr() or out.scales.data_ptr() == out_t.scales.data_ptr()):
+        raise ValueError("%s: out and out_t share memory" % where)
     if noise is not None and (not isinstance(noise, torch.Tensor) or noise.dtype != torch.uint8 or noise.shape != src.shape or noise.device != dev
                               or (cols > 1 and noise.stride(1) != 1)):
         raise ValueError("%s: noise must be a uint8 tensor of src's shape on %s with a contiguous last axis" % (where, dev))

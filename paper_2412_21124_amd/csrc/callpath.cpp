@@ -518,6 +518,7 @@ PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const nt_mx* out = a[2] == Py_None ? nullptr : mx_of(a[2], device, src.rows, src.cols);
     const nt_mx* out_t = a[3] == Py_None ? nullptr : mx_of(a[3], device, src.cols, src.rows);
     if (!out && !out_t) throw Refused();
+    if (out && out_t && src.rows * src.cols > 0 && (out->codes == out_t->codes || out->scales == out_t->scales)) throw Refused();
     const uint32_t flags = truth(a[4]) ? NT_MX_FIT : 0u;
     const uint8_t* noise = nullptr;
     int64_t noise_ld = 0;
