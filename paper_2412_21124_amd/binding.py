@@ -1019,6 +1019,8 @@ def _fresh(shape, dtype, dev, stream) -> torch.Tensor:
 
 def normtest_mx_matmul_workspace_bytes(a: MxTensor, b: MxTensor, dtype: torch.dtype = torch.bfloat16) -> int:
     """Bytes that normtest_mx_matmul(a, b) into a result of this type works in; often 0."""
+    if dtype not in _LIST_DTYPES:
+        raise TypeError("normtest_mx_matmul_workspace_bytes: dtype must be float32, bfloat16 or float16, got %s" % dtype)
     return int(lib().normtest_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols, a.format, b.format, _LIST_DTYPES[dtype]))
 
 

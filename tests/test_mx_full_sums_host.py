@@ -96,3 +96,13 @@ def test_refusals():
     need = L.normtest_mx_matmul_workspace_bytes(64, 64, 1 << 20, B.NT_MX_E4M3, B.NT_MX_E2M1, BF16)
     long = dict(M=64, N=64, K=1 << 20, ld=64)
     assert need > 0 and full(**long) == SMALL and full(**long, workspace=0x8000, size=need - 1) == SMALL and full(**long, workspace=0x8008, size=need) == BAD
+
+
+def test_workspace_of_another_type():
+    """A type that no result has is refused like those of the other calls."""
+    from test_mx_replaced_host import bytes_
+    a = B.MxTensor(bytes_(32, 32), bytes_(32, 16), 32, B.NT_MX_E4M3)
+    assert B.normtest_mx_matmul_workspace_bytes(a, a) == 0
+    for dtype in (B.torch.float64, B.torch.uint8, None):
+        with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+            B.normtest_mx_matmul_workspace_bytes(a, a, dtype)
