@@ -854,6 +854,7 @@ class MxTensor:
 
     codes, scales: uint8 device tensors with a row for every row, of at least ceil(cols / 32) blocks' codes (16 or 32 bytes each; rows begin at
     multiples of 16 bytes) and that many scales.  Elements behind column cols in a row's last block are zero codes.  make_mx allocates one.
+    Rows of scales at multiples of 16 bytes, as make_mx makes them, let large products take their faster kernel (8192^3 in 4 bits 311 us for 421 to 454).
     It stays the matrix of the tensors it was made of, whose bytes may change: its attributes are not assigned, and a call on one whose tensors
     have other memory or another shape by now raises."""
 

@@ -1,7 +1,7 @@
 // Microscaled matrices: quantisation, its inverse, and the RMS norm with the residual's addition that writes one, forward and backward;
 // hand-written for gfx950 (MI355X).  The product of such matrices is in mx_matmul.hip.
 //
-// All of it is bound by memory.  A lane holds eight consecutive elements of a row (16 bytes of a 16-bit type: one access), four lanes a block
+// All of it is bound by memory, but for quantisation in both directions.  A lane holds eight consecutive elements of a row (16 bytes of a 16-bit type: one access), four lanes a block
 // of 32, whose largest magnitude goes round the four by quad permutes; codes and scales come from the registers that the row was read into.
 #include "mx.h"
 
@@ -88,9 +88,11 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_rows(QuantizeArgs a, Sprea
 // A tile of 128 x 128 goes through LDS once: rows are quantised from the registers they were loaded into, columns from LDS, two neighbouring ones of 32
 // elements to a thread.  Four threads take a column's four blocks, so that a row of the transpose is written 64 or 128 bytes at a time.  Rows
 // in LDS are 16 bytes longer than they need, and each 32 of them begin 32 or 64 bytes further on, so that the four blocks of a column lie in
-// different banks.  4096 x 4096 in fp32 25 us (3.4 TB/s); 16384 x 8192 in bf16 with random bytes 173, of which their additions, twice for every
-// element, are some 25 more than memory takes.  Tiles of 128: what one writes of a row of the transpose is a whole line of 64 bytes in 4 bits.  They
-// are taken in order of memory: neighbours on one die were slower (16384 x 8192 and back 284 -> 309).
+// different banks.  Nothing is loaded while a tile is converted and stored, and two (fp32) to four blocks fit a CU, so memory is not kept busy: 16384 x 8192
+// in bf16 to 4 bits takes 98 us, call after call, for 64 at the yardstick's rate, and with random bytes 136 for 85 (165 between a layer's other calls);
+// 4096 x 4096 in fp32 26 for 13.  Of the 38 us that random bytes add their own reading is 21, the rest their additions, twice for every element.  Tiles of
+// 128: what one writes of a row of the transpose is a whole line of 64 bytes in 4 bits.  They are taken in order of memory: neighbours on one die were slower
+// (16384 x 8192 and back 284 -> 309).
 template <int DT>
 struct Tile {
   static constexpr int E = type_bytes(DT), PITCH = NT_MX_TILE * E + 16, SHIFT = 16 * E, BYTES = NT_MX_TILE * PITCH + 4 * SHIFT;
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_both(QuantizeArgs a, uint3
 // ---------------------------------------------------------------------------------------------
 // Back to numbers
 // ---------------------------------------------------------------------------------------------
-// Bound by the stores: 16384 x 8192 from 4 bits to bf16 75 us (4.5 TB/s).
+// Bound by the stores: 16384 x 8192 from 4 bits to bf16 72 us (4.7 TB/s).
 template <int DT, int FMT>
 __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_values(const uint8_t* codes, const uint8_t* scales, int64_t code_ld, int64_t scale_ld,
                                                              int64_t cols, char* out, int64_t ld, Spread s) {
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(NT_MX_THREADS) void k_mx_values(const uint8_t* code
 // ---------------------------------------------------------------------------------------------
 // T threads hold a row, V octets each, from its first reading to its codes: x and the residual are read once.  Sums are in an order that
 // the shape alone fixes; the squares' in fp64, so that none overflows or vanishes.
-// Bound by memory: 16384 x 4096 in bf16 with a sum, to 8 bits, 102 us (4.6 TB/s; 97 with results rounded twice); one row of 4096 4.2 us, two trips to
+// Bound by memory: 16384 x 4096 in bf16 with a sum, to 8 bits, 100 to 102 us (4.7 TB/s; 97 with results rounded twice); one row of 4096 4.2 us, two trips to
 // memory with the row's sum between.
 template <int T, class F>
 __device__ inline F row_sum(F x, F* scratch) {   // over the T threads of a row, in all of them; scratch: one sum a wave
@@ -377,7 +379,7 @@ struct BackwardArgs {
 
 // Blocks walk the rows, R at a time, T threads to a row.  A row is read once where its octets fit a thread's registers beside the columns'
 // sums, else twice.  The weight is in LDS: read through the caches for every row it was 2/3 as many bytes again.  With rows side by side the chip is
-// full with 256 blocks, so that few sums are left to join (16384 x 4096 in bf16, both kernels, 137 -> 105 us, 5.1 TB/s; 512 blocks 108).
+// full with 256 blocks, so that few sums are left to join (16384 x 4096 in bf16, both kernels, 137 -> 105 to 107 us, 5.0 TB/s; 512 blocks 108).
 template <int DT, int T, int V, int R>
 __global__ __launch_bounds__(T * R) void k_rms_backward(BackwardArgs a) {
   constexpr int E = type_bytes(DT), COLS = 8 * T * V;

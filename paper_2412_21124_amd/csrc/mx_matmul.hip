@@ -174,7 +174,7 @@ __device__ inline uint32_t by_step(uint32_t w, int g) {
 // a block's four waves (and blockIdx.z) share those out, and are joined through LDS; the others have columns of their own.  Lanes that hold pieces
 // of one row load 64 bytes of it side by side, and one word of scales each, for 512 columns, which then change places.  (Four blocks of a lane side by
 // side need no change, but every lane loads from a cache line of its own: 24 x 50257 x 768 19.7 us.)  Bound by memory where there is one row (1 x 16384 x
-// 4096 8.2 us, 4.4 TB/s), by the time of a wave, load to last product, where there are more.  Hence U = 2 for fewer than 2048 columns: 24 x 50257 x 768 13.4 ->
+// 4096 8.4 us, 4.3 TB/s), by the time of a wave, load to last product, where there are more.  Hence U = 2 for fewer than 2048 columns: 24 x 50257 x 768 13.4 ->
 // 12.7, of 1536 21.7 -> 19.6 (8 x 50257 x 1024 8.4 -> 8.7).  Blocks side by side are on one die, where the lines that they share are written once: 12.7 -> 12.2,
 // the single row 8.4 to 8.8 -> 8.2.
 template <int F, bool WIDE, int U>
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(64 * NT_MM_THIN_WAVES) void k_mm_thin(MatmulArgs a,
 // A row of LDS has 64 or 128 bytes without a gap (what goes there directly lies as the lanes do), so 16-byte pieces of neighbouring rows change places
 // by the row's number: 16 lanes that read one piece of 16 rows then meet all banks.
 // Below 256 tiles the columns are in parts, as many as 512 blocks (two to a CU) allow: 768 x 2304 x 16384 widened, 108 tiles, four parts 73.8 us, three
-// 85, six 88, nine 84.  There the matrix cores (0.8 of 1.37 PF/s) share the time with widening (20 %).
+// 85, six 88, nine 84.  There the matrix cores (0.8 PF/s, a library's product in bf16 1.6) share the time with widening (20 %).
 template <int FA, int FB>
 constexpr int step_columns() {
   return FA == NT_MX_E2M1 && FB == NT_MX_E2M1 ? 256 : 128;
@@ -523,8 +523,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t
 
 // The same for many tiles: 256 x 256 by eight waves, one block to a CU, steps of 128 columns in a ring of two to four stages, all but one of which are
 // on their way.  Scales, 16 bytes a row for four steps, go to LDS directly too, which asks for rows of scales at multiples of 16 bytes.
-// From 192 tiles on, three quarters of the CUs: 8192^3 in 4 bits 308 us (3.6 PF/s), by tiles of 128 350; 8192 x 16384 x 4096 in 8 x 4 bits 512 and 627.  Bound
-// by the way from cache to LDS: of 296 us in 4 bits the loads alone take 184, the products alone 187, and they overlap by a third.
+// From 192 tiles on, three quarters of the CUs: 8192^3 in 4 bits 311 us (3.5 PF/s), by tiles of 128 401; 8192 x 16384 x 4096 in 8 x 4 bits 499 and 643; 8192^3 in
+// 8 bits 492 and 670 (boxes differ by 5 %).  Bound by the way from cache to LDS and by its place behind the products: in a run of 296 us in 4 bits the loads alone
+// took 184, the products alone 187, and they overlapped by a third.
 template <int FA, int FB>
 struct LargeShape {
   static constexpr int TILE = 256, WM = 2, WN = 4, WAVES = WM * WN, THREADS = 64 * WAVES, STEP = 128, STEPS = NT_MM_CHUNK / STEP;
