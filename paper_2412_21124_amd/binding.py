@@ -855,8 +855,10 @@ class MxTensor:
     codes, scales: uint8 device tensors with a row for every row, of at least ceil(cols / 32) blocks' codes (16 or 32 bytes each; rows begin at
     multiples of 16 bytes) and that many scales.  Elements behind column cols in a row's last block are zero codes.  make_mx allocates one.
     Rows of scales at multiples of 16 bytes, as make_mx makes them, let large products take their faster kernel (8192^3 in 4 bits 311 us for 421 to 454).
-    It stays the matrix of the tensors it was made of, whose bytes may change: its attributes are not assigned, and a call on one whose tensors
+    It stays the matrix of the tensors it was made of, whose bytes may change: these attributes are not assigned, and a call on one whose tensors
     have other memory or another shape by now raises."""
+
+    _FIXED = frozenset(("codes", "scales", "rows", "cols", "format", "device", "native", "_record", "_made_of"))
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, format: int = NT_MX_E2M1):
         if format not in _MX_BLOCK_BYTES:
@@ -887,7 +889,7 @@ class MxTensor:
         self.native = _fast and _fast.make_mx(codes, scales, self.rows, cols, ld, scale_ld, format) or None   # as the native call path knows it
 
     def __setattr__(self, name, value):
-        if "native" in self.__dict__:   # the last one: whole.  What the calls know this matrix by would not follow
+        if name in self._FIXED and "native" in self.__dict__:   # the last one: whole.  What the calls know this matrix by would not follow
             raise AttributeError("a microscaled matrix stays what it was made as: make another MxTensor for other %s" % name)
         super().__setattr__(name, value)
 

@@ -37,3 +37,16 @@ def test_changed_in_place(which, change):
     change(getattr(m, which))
     with pytest.raises(RuntimeError, match="other memory or another shape"):
         m.pointer()
+
+
+def test_other_attributes_are_the_programs_own():
+    class Named(B.MxTensor):
+        def __init__(self, name):
+            super().__init__(bytes_(32, 32), bytes_(32, 32), 32, B.NT_MX_E4M3)
+            self.name = name
+
+    m = Named("up")
+    m.name = m.step = "down"
+    assert m.name == m.step == "down"
+    with pytest.raises(AttributeError, match="make another"):
+        m.scales = bytes_(32, 32)
