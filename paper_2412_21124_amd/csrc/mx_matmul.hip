@@ -524,7 +524,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(MatmulArgs a, uint32_t
 // The same for many tiles: 256 x 256 by eight waves, one block to a CU, steps of 128 columns in a ring of two to four stages, all but one of which are
 // on their way.  Scales, 16 bytes a row for four steps, go to LDS directly too, which asks for rows of scales at multiples of 16 bytes.
 // From 192 tiles on, three quarters of the CUs: 8192^3 in 4 bits 311 us (3.5 PF/s), by tiles of 128 401; 8192 x 16384 x 4096 in 8 x 4 bits 499 and 643; 8192^3 in
-// 8 bits 492 and 670 (boxes differ by 5 %).  Bound by the way from cache to LDS and by its place behind the products: in a run of 296 us in 4 bits the loads alone
+// 8 bits 492 and 670 (cards differ by 5 %).  Bound by the way from cache to LDS and by its place behind the products: in a run of 296 us in 4 bits the loads alone
 // took 184, the products alone 187, and they overlapped by a third.
 template <int FA, int FB>
 struct LargeShape {
